@@ -27,8 +27,7 @@ constexpr int BM = 128, BK = 64;  // rows of an operand tile, and its depth: 128
 constexpr uint32_t kSpinLimit = 1u << 24;
 
 // The two halves of dependent_begin().  A kernel that allocates tensor memory waits for the kernel before it first (so it holds none that
-// that kernel may still need), and lets the next one take its places only after all its blocks have theirs.  What the kernel before writes (c) is
-// read by plain loads: a load of data taken for constant could be moved ahead of the wait.
+// that kernel may still need), and lets the next one take its places only after all its blocks have theirs.  All is read by plain loads (rows.cuh).
 __device__ __forceinline__ void dependent_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -104,8 +103,8 @@ constexpr int kShrinkWarps = 8, kShrinkThreads = 32 * kShrinkWarps;
 __host__ __device__ constexpr size_t shrink_smem(int nt) { return (size_t)(kShrinkWarps / 2) * nt * 128 * sizeof(float); }
 
 template <int NT>
-__global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, const float* __restrict__ X, long long ld, long long f_off, int rank, int width,
-                                                                const bf16* __restrict__ v, long long ld_v, float factor, float* __restrict__ out, int splits) {
+__global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, const float* X, long long ld, long long f_off, int rank, int width,
+                                                                const bf16* v, long long ld_v, float factor, float* out, int splits) {
     dependent_begin();
     extern __shared__ float part[];  // [kShrinkWarps / 2][NT * 4 * 32]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane & 3, row = lane >> 2;
@@ -135,7 +134,7 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
     const uint4 none = make_uint4(0u, 0u, 0u, 0u);
     auto load = [&](int k, uint4 (&a)[2]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) a[i] = k < width ? __ldg(reinterpret_cast<const uint4*>(at[i] + k)) : none;
+        for (int i = 0; i < 2; ++i) a[i] = k < width ? *reinterpret_cast<const uint4*>(at[i] + k) : none;
     };
     const int stride = splits * kShrinkWarps * 32;
     int k = (split * kShrinkWarps + warp) * 32 + 8 * q;
@@ -149,8 +148,8 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
         for (int j = 0; j < NT; ++j) {
             const bool in = 8 * j + row < rank && k < width;
             const float4* p = reinterpret_cast<const float4*>(F + (size_t)(8 * j + row) * width + k);
-            f[j][0] = in ? __ldg(p) : make_float4(0.f, 0.f, 0.f, 0.f);
-            f[j][1] = in ? __ldg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[j][0] = in ? *p : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[j][1] = in ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -374,8 +373,8 @@ __device__ __forceinline__ void land(const Thin<R>& x, int issued) {
 // is its own, theirs are not stored).  The blocks of a cluster share the width.
 // 8192 rows, 4096 wide, rank 16: 20 us (67 MB of rows, 10.2 us of the memory; 3.4 TB/s); rank 64: 32 us, where forming the pieces is as long.
 template <int R>
-__global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid_constant__ CUtensorMap map_v, RowGroups g, const float* __restrict__ X, long long ld, long long f_off,
-                                                                 int rank, int width, float factor, float* __restrict__ out, int splits) {
+__global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid_constant__ CUtensorMap map_v, RowGroups g, const float* X, long long ld, long long f_off,
+                                                                 int rank, int width, float factor, float* out, int splits) {
     using T = Thin<R>;
     extern __shared__ uint8_t raw[];
     if (threadIdx.x == 0) prefetch_map(&map_v);
@@ -419,8 +418,8 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
             const int at = tid + e * T::GROUP_THREADS, j = at >> 3, k = (kb0 + i) * BK + 8 * (at & 7);
             const bool in = i < n && j < rank && k < width;
             const float4* p = reinterpret_cast<const float4*>(F + (size_t)j * width + k);
-            f[e][0] = in ? __ldg(p) : make_float4(0.f, 0.f, 0.f, 0.f);
-            f[e][1] = in ? __ldg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[e][0] = in ? *p : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[e][1] = in ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
         };
 #pragma unroll
         for (int e = 0; e < PER; ++e) load(group, e);
@@ -492,7 +491,7 @@ struct OuterJobs {  // of the one factor, and of the other
     const float* c[2];
 };
 template <int R>
-__global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_constant__ CUtensorMap map_0, const __grid_constant__ CUtensorMap map_1, RowGroups g, float* __restrict__ G,
+__global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_constant__ CUtensorMap map_0, const __grid_constant__ CUtensorMap map_1, RowGroups g, float* G,
                                                                 long long ld, int rank, const __grid_constant__ OuterJobs jobs, int splits) {
     using T = Thin<R>;
     extern __shared__ uint8_t raw[];
@@ -1011,8 +1010,8 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                 const int j = kk - (kk >= R ? R : 0) - (kk >= 2 * R ? R : 0);
                 const bool in = kk < 3 * R && j < a.rank && col < a.N;
                 const float4* p = reinterpret_cast<const float4*>(F + (size_t)j * a.N + col);
-                raw_f[x][0] = in ? __ldg(p) : make_float4(0.f, 0.f, 0.f, 0.f);
-                raw_f[x][1] = in ? __ldg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+                raw_f[x][0] = in ? *p : make_float4(0.f, 0.f, 0.f, 0.f);
+                raw_f[x][1] = in ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
             }
         };
         int tile_extra = 0;
@@ -1087,7 +1086,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                 float bias[32];
                 if (a.bias)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) bias[j] = nb + j < a.N ? __ldg(a.bias + nb + j) : 0.f;
+                    for (int j = 0; j < 32; ++j) bias[j] = nb + j < a.N ? a.bias[nb + j] : 0.f;
                 uint32_t r[32];
                 tc_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + c * 32), r);
                 float v[32];
@@ -1239,7 +1238,7 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
             int lo = 0, hi = a.g.N + 1;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
-                if (__ldg(a.g.rowstart + mid) <= t0 + t) lo = mid + 1;
+                if (a.g.rowstart[mid] <= t0 + t) lo = mid + 1;
                 else hi = mid;
             }
             who[t] = lo - 1 < a.g.N ? lo - 1 : -1;
@@ -1272,14 +1271,14 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
                 float ct[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    f[e] = __ldg(reinterpret_cast<const float4*>(F + (size_t)(j + e) * a.N));
+                    f[e] = *reinterpret_cast<const float4*>(F + (size_t)(j + e) * a.N);
                     ct[e] = c[j + e];
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) add(ct[e], f[e]);
             }
 #pragma unroll 4
-            for (; j < a.rank; ++j) add(c[j], __ldg(reinterpret_cast<const float4*>(F + (size_t)j * a.N)));
+            for (; j < a.rank; ++j) add(c[j], *reinterpret_cast<const float4*>(F + (size_t)j * a.N));
             low[i] = sum;
         }
         if (n > 0) {
@@ -1314,7 +1313,7 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
         for (int i = 0; i < MINE; ++i) {
             const int at = 8 * i + warp - 2, t = split * share + at;
             if (at >= share || t >= rows || n4 >= a.N || who[t] < 0) continue;
-            float4 sum = a.bias ? make_float4(__ldg(a.bias + n4), __ldg(a.bias + n4 + 1), __ldg(a.bias + n4 + 2), __ldg(a.bias + n4 + 3)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 sum = a.bias ? make_float4(a.bias[n4], a.bias[n4 + 1], a.bias[n4 + 2], a.bias[n4 + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
             for (int s = 0; s < splits; ++s) {
                 const float4 v = *reinterpret_cast<const float4*>(sums + (s * share + at) * BM + 4 * lane);
                 sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);

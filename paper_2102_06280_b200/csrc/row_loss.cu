@@ -215,7 +215,7 @@ struct Cut {
 
 // Row t's weight: the caller's, or 1 / rows of its worker (0 where a malformed rowstart gives it none).  All lanes of a warp.
 __device__ __forceinline__ float weight_of(const LossArgs& a, int t) {
-    if (a.row_weight) return __ldg(a.row_weight + t);
+    if (a.row_weight) return a.row_weight[t];
     const int w = worker_of_row(a.g, t);
     if (w < 0) return 0.f;
     const int2 own = rows_of(a.g, w);
@@ -360,8 +360,8 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
             v[k] = -1;
             et[k] = ez[k] = 0.f;
             if (j < n) {
-                v[k] = __ldg(a.top_idx + (size_t)t * a.top + j);
-                et[k] = __ldg(a.top_logit + (size_t)t * a.top + j);
+                v[k] = a.top_idx[(size_t)t * a.top + j];
+                et[k] = a.top_logit[(size_t)t * a.top + j];
                 if (v[k] < -1 || v[k] >= V) {
                     atomicOr(a.g.status, DBW_STATUS_BAD_INDEX);
                     v[k] = -1;
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
         }
         live = __any_sync(0xffffffffu, some);
     } else if (live) {
-        v[0] = __ldg(a.action + t);
+        v[0] = a.action[t];
         live = v[0] >= 0 && v[0] < V;
         if (live) ez[0] = (float)z[v[0]];
         else if (lane == 0) atomicOr(a.g.status, DBW_STATUS_BAD_INDEX);
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
 
     float f, slope = 0.f, p[PER];
     if (KIND == POLICY) {
-        const Policy r(a, ez[0], __ldg(a.old_logp + t), a.kl != 0.f ? __ldg(a.ref_logp + t) : 0.f, __ldg(a.advantage + t), x, c, far);
+        const Policy r(a, ez[0], a.old_logp[t], a.kl != 0.f ? a.ref_logp[t] : 0.f, a.advantage[t], x, c, far);
         if (lane == 0) {
             a.row_loss[t] = r.loss;
             if (a.logp) a.logp[t] = r.logp;
@@ -598,8 +598,8 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
                 v[i] = -1;
                 et[i] = ez[i] = ep[i] = 0.f;
                 if (j < a.top) {
-                    v[i] = __ldg(a.top_idx + (size_t)t * a.top + j);
-                    et[i] = __ldg(a.top_logit + (size_t)t * a.top + j);
+                    v[i] = a.top_idx[(size_t)t * a.top + j];
+                    et[i] = a.top_logit[(size_t)t * a.top + j];
                     if (v[i] < -1 || v[i] >= V) {
                         atomicOr(a.g.status, DBW_STATUS_BAD_INDEX);
                         v[i] = -1;
@@ -627,15 +627,15 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
                 }
             }
         } else {
-            v[0] = __ldg(a.action + t);
+            v[0] = a.action[t];
             asked = v[0] >= 0 && v[0] < V;
             if (asked) ez[0] = (float)z[v[0]];
             else if (lane == 0) atomicOr(a.g.status, DBW_STATUS_BAD_INDEX);
             if (lane == 0) {
                 info.z = asked ? ez[0] : 0.f;
-                info.old = __ldg(a.old_logp + t);
-                info.ref = a.kl != 0.f ? __ldg(a.ref_logp + t) : 0.f;
-                info.adv = __ldg(a.advantage + t);
+                info.old = a.old_logp[t];
+                info.ref = a.kl != 0.f ? a.ref_logp[t] : 0.f;
+                info.adv = a.advantage[t];
             }
         }
         if (lane == 0) info.asked = asked;
@@ -789,14 +789,14 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
 }
 
 // loss[w] = sum of weight x row_loss over the worker's rows, in an order that depends on their number alone.  A block per worker.
-__global__ void __launch_bounds__(kThreads) worker_loss_kernel(RowGroups g, const float* __restrict__ row_weight, const float* row_loss, float* __restrict__ loss) {
+__global__ void __launch_bounds__(kThreads) worker_loss_kernel(RowGroups g, const float* row_weight, const float* row_loss, float* loss) {
     dependent_begin();
     __shared__ double part[kThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int2 own = rows_of(g, blockIdx.x);
     double sum = 0.0;
     for (int t = own.x + threadIdx.x; t < own.y; t += kThreads) {
-        const float w = row_weight ? __ldg(row_weight + t) : 1.f;
+        const float w = row_weight ? row_weight[t] : 1.f;
         if (w != 0.f) sum += (double)w * (double)row_loss[t];
     }
 #pragma unroll

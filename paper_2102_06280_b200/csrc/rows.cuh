@@ -1,5 +1,9 @@
 // Rows of a batch grouped by worker: rowstart[w] .. rowstart[w+1]-1 are worker w's.  Shared by the adapter and the
 // vocabulary-loss kernels.  Whatever rowstart holds, the ranges handed out lie within [0, rows].
+//
+// The kernels that use this start while the one before them on the stream still runs (dependent_begin).  What that one may write changes while they
+// live, and for data that changes the constant-cache load (ld.global.nc: __ldg, or a const pointer that is __restrict__) promises nothing, be it issued
+// before the wait or behind it.  So they read their arrays by plain loads, whoever wrote them.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -15,7 +19,7 @@ struct RowGroups {
     uint32_t* status;
 };
 
-__device__ __forceinline__ int row_bound(const RowGroups& g, int w) { return min(max(__ldg(g.rowstart + w), 0), g.rows); }
+__device__ __forceinline__ int row_bound(const RowGroups& g, int w) { return min(max(g.rowstart[w], 0), g.rows); }
 __device__ __forceinline__ int2 rows_of(const RowGroups& g, int w) {
     const int a = row_bound(g, w), b = row_bound(g, w + 1);
     return make_int2(a, max(a, b));
@@ -25,8 +29,8 @@ __device__ __forceinline__ int2 rows_of(const RowGroups& g, int w) {
 __device__ __forceinline__ void check_groups(const RowGroups& g) {
     bool bad = false;
     for (int w = threadIdx.x; w <= g.N; w += blockDim.x) {
-        const int a = __ldg(g.rowstart + w);
-        bad |= a < 0 || a > g.rows || (w < g.N && __ldg(g.rowstart + w + 1) < a);
+        const int a = g.rowstart[w];
+        bad |= a < 0 || a > g.rows || (w < g.N && g.rowstart[w + 1] < a);
     }
     if (bad) atomicOr(g.status, DBW_STATUS_BAD_INDEX);
 }
@@ -38,7 +42,7 @@ __device__ __forceinline__ int worker_of_row(const RowGroups& g, int t) {
     int lo = 0, hi = g.N + 1;  // c lies in [lo, hi]
     while (lo < hi) {
         const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-        const int k = __popc(__ballot_sync(0xffffffffu, at < hi && __ldg(g.rowstart + at) <= t));
+        const int k = __popc(__ballot_sync(0xffffffffu, at < hi && g.rowstart[at] <= t));
         hi = min(hi, lo + (k + 1) * step - 1);
         lo = lo + k * step;
     }
