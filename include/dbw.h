@@ -397,7 +397,9 @@ int dbw_lowrank_backward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, 
  *             without rows; d_logits (nullable: loss only) [rows] rows of `vocab` values of `type`, ld_d elements apart: the gradient
  *             of loss[w] with respect to the row's logits.  d_logits may be logits itself (same ld): then the gradient replaces them.
  * q = softmax(logits / temperature) over the vocabulary, temperature 1e-15 .. 1e15; a logit of -inf has q = 0 and a gradient of 0 (plus what the teacher or
- * the action asks for).  A row of weight other than 0 with a NaN, a +inf or nothing but -inf gives NaN.
+ * the action asks for).  A row of weight other than 0 with a NaN, a +inf or nothing but -inf gives NaN.  What passes the range of fp32 is infinite: a
+ * ratio or a KL term beyond 2^128 gives an infinite slope, and with it an infinite gradient (NaN where q, or for the action 1 - q, has
+ * underflowed; a logit of -inf keeps its 0).
  *
  * dbw_distill: distillation from a teacher of which only each row's top logits are known.
  *     p = softmax(top_logit / temperature) over the row's entries,

@@ -284,6 +284,13 @@ struct Policy {
     }
 };
 
+// The gradient's factor f times the power e of a logit z.  An infinite f (a slope beyond fp32: a ratio or a KL term of more than 2^128) leaves a logit
+// of -inf without a gradient; times another power that has become 0 it is NaN, the product being anything.
+__device__ __forceinline__ bool infinite(float f) { return fabsf(f) == INFINITY; }
+__device__ __forceinline__ float share(float f, float e, float z) { return z == -INFINITY && infinite(f) ? 0.f : f * e; }
+// The action's own: slope (1 - e / S), f = -slope / S; an infinite one stays where q < 1 (and is NaN at 1, as above).
+__device__ __forceinline__ float action_share(float slope, float f, float e, float S) { return infinite(slope) && e < S ? slope : slope + f * e; }
+
 // What L2 keeps: logits that are read a second time stay; their second reading and the gradient are the first to leave.
 __device__ __forceinline__ uint64_t keep_policy() {
     uint64_t p;
@@ -448,26 +455,24 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
     if (!d) return;
     __syncwarp();  // the gradient may replace the logits: all that is wanted of them has been read
     const uint64_t leave = leave_policy();
+    const bool slow = far || infinite(f);
 #pragma unroll
     for (int k = 0; k < HELD; ++k) {
         if (lane + 32 * k >= cut.pieces) continue;
         float g[VN];
-        if (far) {
+        if (slow) {
             Vec<T>::load(held[k], g);
 #pragma unroll
-            for (int e = 0; e < VN; ++e) g[e] = f * power_beyond(g[e], m, c);
+            for (int e = 0; e < VN; ++e) g[e] = share(f, at_row(g[e]), g[e]);
         } else {
             grade_piece<T>(held[k], cm, c, f, g);
         }
         put(d, cut.head + (lane + 32 * k) * VN, alike, g, leave);
     }
-    if (lane < cut.loose) d[cut.loose_at(lane)] = T(f * at_row(loose));
+    if (lane < cut.loose) d[cut.loose_at(lane)] = T(share(f, at_row(loose), loose));
     __syncwarp();
     if (KIND == POLICY) {
-        if (lane == 0) {
-            const float e = at_row(ez[0]);
-            d[v[0]] = T(slope + (e == 0.f ? 0.f : f * e));  // an action that the policy rules out: its slope alone, infinite though it may be
-        }
+        if (lane == 0) d[v[0]] = T(action_share(slope, f, at_row(ez[0]), x.s));
     } else {
         const float scale = weight * (float)a.tau;
 #pragma unroll
@@ -476,7 +481,7 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
             float sum = 0.f;  // of every entry of this index
             for (int i = 0; i < n; ++i)
                 if (entry_v[slot][i] == v[k]) sum += entry_p[slot][i];
-            d[v[k]] = T(fmaf(-scale, sum, f * at_row(ez[k])));
+            d[v[k]] = T(fmaf(-scale, sum, share(f, at_row(ez[k]), ez[k])));
         }
     }
 }
@@ -756,7 +761,7 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
             }
             out += P * G * VN;
         };
-        if (!far) {
+        if (!far && !infinite(f)) {
             uint4 u[P];
             for (int i = 0; i < whole; ++i) {
                 next(u);
@@ -767,23 +772,23 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
                 write(u, last_pieces);
             }
         } else {
-            for (int i = cut.head + tid; i < cut.head + cut.pieces * VN; i += G) d[i] = T(f * power_beyond((float)z[i], m, c));
+            for (int i = cut.head + tid; i < cut.head + cut.pieces * VN; i += G) {
+                const float y = (float)z[i];
+                d[i] = T(share(f, at_row(y), y));
+            }
         }
-        if (tid < cut.loose) d[cut.loose_at(tid)] = T(f * at_row(info.loose[tid]));
+        if (tid < cut.loose) d[cut.loose_at(tid)] = T(share(f, at_row(info.loose[tid]), info.loose[tid]));
         asm volatile("cp.async.wait_all;" ::: "memory");
         asm volatile("bar.arrive 1, %0;" ::"n"(G + 32) : "memory");
     } else {
         asm volatile("bar.sync 1, %0;" ::"n"(G + 32) : "memory");
         if (KIND == POLICY) {
-            if (lane == 0) {
-                const float e = at_row(ez[0]);
-                d[v[0]] = T(slope + (e == 0.f ? 0.f : f * e));  // an action that the policy rules out: its slope alone, infinite though it may be
-            }
+            if (lane == 0) d[v[0]] = T(action_share(slope, f, at_row(ez[0]), x.s));
         } else {
             const float scale = weight * (float)a.tau;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                if (v[i] >= 0) d[v[i]] = T(fmaf(-scale, ep[i], f * at_row(ez[i])));
+                if (v[i] >= 0) d[v[i]] = T(fmaf(-scale, ep[i], share(f, at_row(ez[i]), ez[i])));
         }
     }
 }
