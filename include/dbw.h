@@ -346,11 +346,13 @@ int dbw_graph_order_2of4(int32_t N, const int32_t* h_rowptr, const int32_t* h_co
 #define DBW_TYPE_F16 2
 
 #define DBW_LOWRANK_MAX_RANK 64
+#define DBW_LOWRANK_MAX_WIDTH (1 << 30)
+#define DBW_MAX_ROWS ((1 << 30) - 4096) /* of a batch; more: DBW_ERR_TOO_LARGE (a row's number is a sum of two such in 32 bits) */
 
 /* One projection in -> out with an adapter of the given rank: worker w's factors A_w [rank][in] and B_w [rank][out] (fp32,
  * row-major) lie at float offsets a_off and b_off of row w of X, and their gradients there in G. */
 typedef struct {
-    int32_t in, out; /* multiples of 8 */
+    int32_t in, out; /* multiples of 8, DBW_LOWRANK_MAX_WIDTH at most */
     int32_t rank;    /* 1 .. DBW_LOWRANK_MAX_RANK */
     int64_t a_off, b_off; /* multiples of 32 */
 } dbw_lowrank_desc;

@@ -186,8 +186,12 @@ bool disjoint(const Span (&in)[I], const Span (&out)[O]) {
     return true;
 }
 
+bool valid_shape(const dbw_lowrank_desc& a) {
+    auto width = [](int32_t n) { return n >= 8 && n <= DBW_LOWRANK_MAX_WIDTH && !(n & 7); };
+    return width(a.in) && width(a.out) && a.rank >= 1 && a.rank <= DBW_LOWRANK_MAX_RANK;
+}
 bool valid_lowrank(const dbw_handle* h, const dbw_lowrank_desc* a) {
-    if (a->in < 8 || a->out < 8 || (a->in & 7) || (a->out & 7) || a->rank < 1 || a->rank > DBW_LOWRANK_MAX_RANK) return false;
+    if (!valid_shape(*a)) return false;
     if (a->a_off < 0 || a->b_off < 0 || (a->a_off & 31) || (a->b_off & 31)) return false;
     const int64_t na = (int64_t)a->rank * a->in, nb = (int64_t)a->rank * a->out;
     if (na > h->ld || nb > h->ld || a->a_off > h->ld - na || a->b_off > h->ld - nb) return false;
@@ -199,6 +203,7 @@ bool valid_rows(const void* p, int64_t ld, int32_t width) { return aligned16(p) 
 // What the losses over a vocabulary check alike.  `more`: the further inputs of the loss at hand.
 int check_row_loss(const dbw_handle* h, const RowLoss& r, const Span (&more)[4], const Span& extra_out) {
     if (!h || !r.rowstart || (r.rows > 0 && (!r.logits || !r.row_loss))) return DBW_ERR_NULL;
+    if (r.rows > DBW_MAX_ROWS) return DBW_ERR_TOO_LARGE;
     const size_t size = r.type == DBW_TYPE_F32 ? 4 : 2;
     if (r.type < DBW_TYPE_F32 || r.type > DBW_TYPE_F16 || r.rows < 0 || r.vocab < 1 || r.vocab > 1 << 30 || r.ld < r.vocab || r.ld >= (int64_t)1 << 38 ||
         (r.d_logits && (r.ld_d < r.vocab || r.ld_d >= (int64_t)1 << 38)) || ((uintptr_t)r.logits & (size - 1)) || ((uintptr_t)r.d_logits & (size - 1)))
@@ -684,7 +689,7 @@ int dbw_lowrank_layout(const int32_t* shapes, int32_t n, dbw_lowrank_desc* desc,
         a.in = shapes[3 * k];
         a.out = shapes[3 * k + 1];
         a.rank = shapes[3 * k + 2];
-        if (a.in < 8 || a.out < 8 || (a.in & 7) || (a.out & 7) || a.rank < 1 || a.rank > DBW_LOWRANK_MAX_RANK) return DBW_ERR_BAD_MODEL;
+        if (!valid_shape(a)) return DBW_ERR_BAD_MODEL;
         a.a_off = off;
         off = round32(off + (int64_t)a.rank * a.in);
         a.b_off = off;
@@ -700,6 +705,7 @@ int dbw_lowrank_forward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, c
                         const int32_t* rowstart, int32_t rows, void* y, int64_t ld_y, float* hidden, void* stream) {
     if (!h || !a || !X || !W || !rowstart || (rows > 0 && (!x || !y || !hidden))) return DBW_ERR_NULL;
     if (!valid_lowrank(h, a)) return DBW_ERR_BAD_MODEL;
+    if (rows > DBW_MAX_ROWS) return DBW_ERR_TOO_LARGE;
     if (rows < 0 || !valid_rows(x, ld_x, a->in) || !valid_rows(y, ld_y, a->out) || !aligned16(X) || !aligned16(W) || !aligned16(hidden)) return DBW_ERR_BAD_SHAPE;
     const Span in[] = {span(X, (size_t)h->N * h->ld * 4), span(W, (size_t)a->in * a->out * 2), span(bias, (size_t)a->out * 4),
                        span(x, strided(rows, ld_x, a->in, 2)), span(rowstart, ((size_t)h->N + 1) * 4)};
@@ -713,6 +719,7 @@ int dbw_lowrank_backward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, 
                          const void* dy, int64_t ld_dy, const int32_t* rowstart, int32_t rows, float* G, float* d_hidden, void* dx, int64_t ld_dx, void* stream) {
     if (!h || !a || !X || !W || !rowstart || !G || (rows > 0 && (!x || !hidden || !dy || !d_hidden))) return DBW_ERR_NULL;
     if (!valid_lowrank(h, a)) return DBW_ERR_BAD_MODEL;
+    if (rows > DBW_MAX_ROWS) return DBW_ERR_TOO_LARGE;
     if (rows < 0 || !valid_rows(x, ld_x, a->in) || !valid_rows(dy, ld_dy, a->out) || (dx && !valid_rows(dx, ld_dx, a->in)) || !aligned16(X) || !aligned16(W) ||
         !aligned16(G) || !aligned16(hidden) || !aligned16(d_hidden))
         return DBW_ERR_BAD_SHAPE;
