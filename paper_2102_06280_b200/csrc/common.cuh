@@ -369,6 +369,7 @@ struct RowLoss {  // what the losses over a vocabulary have in common
     void* d_logits;
     int64_t ld_d;
 };
+int launch_check_groups(dbw_handle* h, const int32_t* rowstart, int32_t rows, cudaStream_t s);  // for calls whose kernels would not: those without rows
 int launch_distill(dbw_handle* h, const RowLoss& r, const int32_t* top_idx, const float* top_logit, int top, cudaStream_t s);
 int launch_policy_loss(dbw_handle* h, const RowLoss& r, const int32_t* action, const float* old_logp, const float* ref_logp, const float* advantage,
                        float clip_low, float clip_high, float kl_coef, float* logp, cudaStream_t s);

@@ -1480,7 +1480,7 @@ int launch_outer(dbw_handle* h, const RowGroups& g, float* G, int rank, const Ou
 
 int launch_lowrank_forward(dbw_handle* h, const dbw_lowrank_desc& a, float scale, const float* X, const void* W, const float* bias, const void* x,
                            int64_t ld_x, const int32_t* rowstart, int32_t rows, void* y, int64_t ld_y, float* hidden, cudaStream_t s) {
-    if (rows == 0) return DBW_OK;
+    if (rows == 0) return launch_check_groups(h, rowstart, rows, s);
     const RowGroups g{rowstart, h->N, rows, h->d_status};
     const int rc = launch_shrink(h, g, X, a.a_off, a.rank, a.in, x, ld_x, 1.f, hidden, s);
     if (rc) return rc;
@@ -1492,7 +1492,7 @@ int launch_lowrank_backward(dbw_handle* h, const dbw_lowrank_desc& a, float scal
                             int64_t ld_dx, cudaStream_t s) {
     const RowGroups g{rowstart, h->N, rows, h->d_status};
     int rc;
-    if (rows > 0 && (rc = launch_shrink(h, g, X, a.b_off, a.rank, a.out, dy, ld_dy, scale, d_hidden, s))) return rc;
+    if ((rc = rows > 0 ? launch_shrink(h, g, X, a.b_off, a.rank, a.out, dy, ld_dy, scale, d_hidden, s) : launch_check_groups(h, rowstart, rows, s))) return rc;
     if ((rc = launch_outer(h, g, G, a.rank, {a.b_off, a.out, dy, ld_dy, scale, hidden}, {a.a_off, a.in, x, ld_x, 1.f, d_hidden}, s))) return rc;
     if (!dx || rows == 0) return DBW_OK;
     return launch_project<true>(h, {g, X, h->ld, a.a_off, a.rank, a.in, a.out, 1.f, d_hidden, nullptr, (bf16*)dx, ld_dx}, W, dy, ld_dy, s);

@@ -793,6 +793,11 @@ __global__ void __launch_bounds__(G + 32, Stream<G>::BLOCKS) long_row_kernel(con
     }
 }
 
+__global__ void __launch_bounds__(kThreads) check_groups_kernel(RowGroups g) {
+    dependent_begin();
+    check_groups(g);
+}
+
 // loss[w] = sum of weight x row_loss over the worker's rows, in an order that depends on their number alone.  A block per worker.
 __global__ void __launch_bounds__(kThreads) worker_loss_kernel(RowGroups g, const float* row_weight, const float* row_loss, float* loss) {
     dependent_begin();
@@ -831,7 +836,10 @@ int launch_long(dbw_handle* h, const LossArgs& a, cudaStream_t s) {
 
 template <class T, int KIND>
 int launch_rows(dbw_handle* h, const LossArgs& a, float* loss, cudaStream_t s) {
-    if (a.g.rows > 0) {
+    if (a.g.rows == 0) {
+        const int rc = launch_check_groups(h, a.g.rowstart, 0, s);
+        if (rc) return rc;
+    } else {
         // A warp where a row fits its registers; else a block of 128, 256 or 512 threads, by the bytes of a row (us, 128 / 256 / 512: rows of
         // 26 KB 175 / 231 / -, 62 KB 53 / 47 / 51, 98 KB - / 91 / 95, 250 KB - / 473 / 430).
         const int64_t bytes = (int64_t)a.vocab * sizeof(T);
@@ -862,6 +870,12 @@ int launch_type(dbw_handle* h, const LossArgs& a, int type, float* loss, cudaStr
 }
 
 }  // namespace
+
+int launch_check_groups(dbw_handle* h, const int32_t* rowstart, int32_t rows, cudaStream_t s) {
+    launch(check_groups_kernel, 1, kThreads, 0, s, RowGroups{rowstart, h->N, rows, h->d_status});
+    DBW_LAUNCHED();
+    return DBW_OK;
+}
 
 int launch_distill(dbw_handle* h, const RowLoss& r, const int32_t* top_idx, const float* top_logit, int top, cudaStream_t s) {
     LossArgs a{{r.rowstart, h->N, r.rows, h->d_status}, r.logits, r.ld, r.vocab, r.row_weight, r.row_loss, r.d_logits, r.ld_d, (double)r.temperature, 1.0 / (double)r.temperature};

@@ -43,3 +43,27 @@ def test_policy_slopes_beyond_fp32(kind, vocab, more):
     assert torch.isfinite(d[rest]).all() and torch.isfinite(q.row_loss[rest]).all()
     assert torch.isposinf(q.row_loss[[0, 1, 4, 5]]).all() and torch.isfinite(q.row_loss[2])
     assert q.h.status() == 0
+
+
+@pytest.mark.parametrize("bad", [[0, 0, 1], [-1, 0, 0], [1, 0, 0], [5, 5, 5]])
+def test_bad_ranges_of_a_batch_without_rows_are_reported(bad):
+    import paper_2102_06280_b200 as p
+    q, z = Projection([0, 0], 64, 32, 4), Loss([0, 0], 100)
+    rs = dev(np.array(bad, dtype=np.int32))
+
+    def policy(loss):
+        none = torch.zeros(0, device="cuda")
+        z.h.policy_loss(z.z, none.int(), none, none, z.rs, none, loss=loss)
+
+    def distill(loss):
+        z.h.distill(z.z, torch.zeros(0, 5, device="cuda", dtype=torch.int32), torch.zeros(0, 5, device="cuda"), z.rs, torch.zeros(0, device="cuda"), loss=loss)
+
+    for h, call in ((q.h, q.forward), (q.h, q.backward), (z.h, lambda: policy(None)), (z.h, lambda: policy(z.loss)), (z.h, lambda: distill(None)), (z.h, lambda: distill(z.loss))):
+        q.rs, z.rs = dev(q.rowstart), dev(z.rowstart)
+        call()
+        assert h.status() == 0
+        q.rs = z.rs = rs
+        call()
+        torch.cuda.synchronize()
+        assert h.status() == p.STATUS_BAD_INDEX
+    assert (q.G[:, q.ad.a_off: q.ad.a_off + 256] == 0).all() and (z.loss == 0).all()
