@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of this turn: what the MMAs add up is truncated, so it goes no further than 32 k
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const float4 x = f[j][half];
@@ -162,8 +163,10 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
                 const uint4 lo = now[0], hi = now[1];
                 const uint32_t a[4] = {half ? lo.z : lo.x, half ? hi.z : hi.x, half ? lo.w : lo.y, half ? hi.w : hi.y};
 #pragma unroll
-                for (int p = 2; p >= 0; --p) mma(acc[j], a, b0[p], b1[p]);
+                for (int p = 2; p >= 0; --p) mma(sum, a, b0[p], b1[p]);
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] += sum[e];
         }
         now[0] = next[0];
         now[1] = next[1];
@@ -207,13 +210,16 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
 // Both are products of few columns (3 R: the pieces of an fp32 operand side by side, R = rank rounded up to 16) with a 128-row
 // operand that is read once, so what bounds them is that reading.  Warp 0 of a block brings the bf16 operand by TMA, one thread of warp 1
 // issues the MMAs (cta_group::1, M = 128, N = 3 R), the others read the fp32 operand, form its pieces in shared memory (128-byte
-// swizzle) and at the end add up the accumulators: those of h, m and l are columns of their own.  Tensor-memory sums are truncated, not
-// rounded, at every MMA (K = 784: -5e-7 of a sum), so the k loop is cut into `sets` runs with accumulators of their own that are
-// added with rounding.
+// swizzle) and add up the accumulators: those of h, m and l are columns of their own.  Tensor-memory sums are truncated, not
+// rounded, at every MMA (K = 784: -5e-7 of a sum), so the k loop is cut into runs of at most kRun stages, which go to the sets of accumulators
+// by turns; who forms pieces moves a run's sums to registers, added there with rounding, before it fills the first stage of the run that
+// takes the set next (the MMAs of the runs between are under way meanwhile, and nobody waits).  Sums of one sign, rank 64: 2.3e-7 short at any length
+// (with runs as long as the sets allow: 131072 values 3.4e-4, 40000 rows 6.9e-5); 8192 rows, 4096 <- 4096, rank 64: 377 us for the backward pass (370).
 // Forming pieces is a chain of loads, roundings, shared-memory writes and a fence, so the warps are four groups and a group fills
 // every fourth stage by itself, the one slot of the ring that is its own (all of them on one stage after another: 8192 rows, 4096 wide,
 // rank 64: shrink 39 us, outer 57).
 constexpr int kFillGroups = 4;
+constexpr int kRun = 8;  // stages: 32 MMAs, 512 k
 __host__ __device__ constexpr int fill_warps(int R) { return R <= 16 ? 8 : 16; }
 __host__ __device__ constexpr int thin_threads(int R) { return 64 + 32 * fill_warps(R); }
 __host__ __device__ constexpr int thin_columns(int R) { return R <= 16 ? 256 : 512; }  // of tensor memory: two blocks an SM, or one
@@ -222,7 +228,7 @@ __host__ __device__ constexpr int thin_set(int R) { return (3 * R + 31) / 32 * 3
 __host__ __device__ constexpr int thin_sets(int R) { return thin_columns(R) / thin_set(R); }
 __host__ __device__ constexpr int thin_b_bytes(int R) { return (3 * R + 63) / 64 * 8192; }  // one stage of pieces: 3 R rows of 64 k, or 64 k rows of 3 R
 __host__ __device__ constexpr size_t thin_ring(int R) { return (size_t)thin_a_stages(R) * (BM * BK * 2) + (size_t)kFillGroups * thin_b_bytes(R); }
-__host__ __device__ constexpr size_t thin_smem(int R) { return thin_ring(R) + 1024 /*alignment*/ + 256 /*barriers*/; }
+__host__ __device__ constexpr size_t thin_smem(int R) { return thin_ring(R) + 1024 /*alignment*/ + 384 /*barriers*/; }
 // kind::f16, D fp32, A and B bf16, M = 128, N = 3 R; bits 15 and 16: A and B MN-major
 __host__ __device__ constexpr uint32_t thin_idesc(int R, bool mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (mn ? 3u << 15 : 0u) | ((uint32_t)(3 * R >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
@@ -264,8 +270,9 @@ struct Thin {
     static constexpr int STAGES = kFillGroups, A_STAGES = thin_a_stages(R), A_BYTES = BM * BK * 2, B_BYTES = thin_b_bytes(R), SET = thin_set(R), SETS = thin_sets(R);
     static constexpr int FILL_WARPS = fill_warps(R), GROUP_THREADS = 32 * FILL_WARPS / kFillGroups, THREADS = thin_threads(R);
     uint8_t *a, *b;
-    // of a stage: its copy is there and has been read, its pieces are there and have been read; the sums are there, and have been read
+    // of a stage: its copy is there and has been read, its pieces are there and have been read; of a set: its sums are there, and have been read
     uint64_t *landed, *used, *filled, *empty, *done, *drained, *shutdown;
+    static_assert((2 * A_STAGES + 2 * STAGES + 2 * SETS + 1) * 8 + 8 <= 384 && R / 16 <= FILL_WARPS / 4, "room for the barriers; a warp has 16 columns of sums at most");
     volatile uint32_t* abort;
     uint32_t tmem, *status;
 
@@ -279,8 +286,8 @@ struct Thin {
         filled = used + A_STAGES;
         empty = filled + STAGES;
         done = empty + STAGES;
-        drained = done + 1;
-        shutdown = drained + 1;
+        drained = done + SETS;
+        shutdown = drained + SETS;
         uint32_t* slot = reinterpret_cast<uint32_t*>(shutdown + 1);
         abort = slot + 1;
         status = status_word;
@@ -294,8 +301,10 @@ struct Thin {
                 mbar_init(&filled[s], FILL_WARPS / kFillGroups);
                 mbar_init(&empty[s], 1);
             }
-            mbar_init(done, 1);
-            mbar_init(drained, FILL_WARPS);
+            for (int s = 0; s < SETS; ++s) {
+                mbar_init(&done[s], 1);
+                mbar_init(&drained[s], FILL_WARPS);
+            }
             mbar_init(shutdown, 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -324,15 +333,21 @@ struct Thin {
         if ((threadIdx.x & 31) == 0) ok = ptx::mbar_wait_bounded<false>(bar, parity, kSpinLimit / 4, pause_ns, abort, status);
         return __all_sync(0xffffffffu, ok);
     }
-    // The MMAs of `n` stages, from ring position `it` on, in runs of `run` to a set.  One thread.
+    static __device__ __forceinline__ int run_of(int n) { return min(kRun, (n + SETS - 1) / SETS); }  // stages of a run, of n in all
+    // The MMAs of `n` stages, from ring position `it` and run number `rt` on.  One thread.
     template <bool MN>
-    __device__ __forceinline__ bool multiply(int it, int n, int run) const {
+    __device__ __forceinline__ bool multiply(int it, int& rt, int n) const {
         using namespace ptx;
         const uint64_t da = MN ? mnmajor_sw128_desc(smem_u32(a), 8192) : kmajor_sw128_desc(smem_u32(a));
         const uint64_t db = MN ? mnmajor_sw128_desc(smem_u32(b), 8192) : kmajor_sw128_desc(smem_u32(b));
         constexpr uint64_t STEP = (MN ? 16 * 128 : 16 * 2) / 16;  // 16 further along k: 16 rows of 128 bytes, or 32 bytes inside the swizzle atom
+        const int run = run_of(n);
         for (int i = 0, in_set = 0, set = 0; i < n; ++i, ++it) {
             const int sa = it % A_STAGES, s = it % STAGES;
+            if (in_set == 0) {
+                set = rt % SETS;
+                if (rt >= SETS && !wait(&drained[set], ((rt / SETS) - 1) & 1)) return false;
+            }
             if (!wait(&landed[sa], (it / A_STAGES) & 1) || !wait(&filled[s], (it / STAGES) & 1)) return false;
             tc_fence_after();
 #pragma unroll
@@ -340,25 +355,38 @@ struct Thin {
                 tc_mma_own(tmem + set * SET, da + (uint64_t)(sa * (A_BYTES / 16)) + k * STEP, db + (uint64_t)(s * (B_BYTES / 16)) + k * STEP, thin_idesc(R, MN), in_set > 0 || k > 0);
             tc_commit_own(&empty[s]);
             tc_commit_own(&used[sa]);
-            if (++in_set == run) {
+            if (++in_set == run || i == n - 1) {
+                tc_commit_own(&done[set]);
                 in_set = 0;
-                ++set;
+                ++rt;
             }
         }
-        tc_commit_own(done);
         return true;
     }
-    // The sums of columns [16 g, 16 g + 16) of the operand that was split, over `sets` sets, in this warp's lane quarter.  All lanes.
-    __device__ __forceinline__ void sums(int g, int sets, float (&v)[16]) const {
+    // Adds the sums of run `rt` to v: columns [16 g, 16 g + 16) of the operand that was split, g being the warp's number in its lane quarter (none
+    // behind the last).  A warp that forms pieces, all lanes; false: a wait ran out.
+    __device__ __forceinline__ bool drain(int rt, float (&v)[16]) const {
+        const int set = rt % SETS, g = (int)(threadIdx.x >> 5) - 2 >> 2;
+        if (!wait_warp(&done[set], (rt / SETS) & 1, 64)) return false;
+        ptx::tc_fence_after();
+        if (g < R / 16) {
+            const uint32_t at = tmem + ((threadIdx.x >> 5 & 3u) << 21) + set * SET + 16 * g;
+            uint32_t r[16];
+            float sum[16];
+            tc_ld16(at + 2 * R, r);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = 0.f;
-        for (int p = 2; p >= 0; --p)
-            for (int set = 0; set < sets; ++set) {
-                uint32_t r[16];
-                tc_ld16(tmem + ((threadIdx.x >> 5 & 3u) << 21) + set * SET + p * R + 16 * g, r);
+            for (int j = 0; j < 16; ++j) sum[j] = __uint_as_float(r[j]);
+            tc_ld16(at + R, r);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] += __uint_as_float(r[j]);
-            }
+            for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(r[j]);
+            tc_ld16(at, r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] += sum[j] + __uint_as_float(r[j]);
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&drained[set]);
+        return true;
     }
 };
 
@@ -388,8 +416,10 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
     dependents_may_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = blockIdx.x % splits;
     const int all = (width + BK - 1) / BK, kb0 = (int)((long long)all * split / splits), n = (int)((long long)all * (split + 1) / splits) - kb0;
-    const int run = (n + T::SETS - 1) / T::SETS;
     bool live = true;
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.f;
     if (warp == 0) {
         if (lane == 0) {
             int i = 0;
@@ -405,7 +435,8 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
             if (!live) land(x, i);
         }
     } else if (warp == 1) {
-        if (lane == 0 && !x.template multiply<false>(0, n, run)) {
+        int rt = 0;
+        if (lane == 0 && !x.template multiply<false>(0, rt, n)) {
             tc_commit_own(x.shutdown);
             ptx::mbar_wait_quiet<false>(x.shutdown, 0, 1u << 20);
         }
@@ -423,9 +454,12 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
         };
 #pragma unroll
         for (int e = 0; e < PER; ++e) load(group, e);
+        const int run = T::run_of(n);
+        int rt = 0;
         for (int i = group; i < n; i += kFillGroups) {
             const int s = i % T::STAGES;
-            if (i >= T::STAGES) live = x.wait_warp(&x.empty[s], ((i / T::STAGES) - 1) & 1, 32);
+            for (; live && i >= (rt + T::SETS) * run; ++rt) live = x.drain(rt, v);
+            if (live && i >= T::STAGES) live = x.wait_warp(&x.empty[s], ((i / T::STAGES) - 1) & 1, 32);
             if (!live) break;
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
@@ -443,8 +477,7 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&x.filled[s]);
         }
-        if (live) live = x.wait_warp(x.done, 0, 64);
-        ptx::tc_fence_after();
+        for (; live && rt * run < n; ++rt) live = x.drain(rt, v);
     }
     // ---- sums: every block of the cluster gets its share of the rows from all of them, over the ring, adds it up and writes it ----
     // (loads from the other blocks instead, one behind the other, took 8 us of 35 at rank 64)
@@ -456,12 +489,10 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
     if (warp >= 2) {
         const int row = (warp & 3) * 32 + lane;
         const uint32_t to = map_to_block(smem_u32(sums + (split * share + row % share) * PITCH), row / share);
-        for (int group = (warp - 2) >> 2; group < R / 16; group += T::FILL_WARPS / 4) {
-            float v[16];
-            x.sums(group, live ? (n + run - 1) / run : 0, v);
+        const int group = (warp - 2) >> 2;
+        if (group < R / 16)
 #pragma unroll
             for (int j = 0; j < 16; j += 4) store_to(to + (16 * group + j) * 4, v[j], v[j + 1], v[j + 2], v[j + 3]);
-        }
     }
     if (splits > 1) cluster_sync();
     else __syncthreads();
@@ -512,8 +543,9 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
         const int all = (r.y - r.x + BK - 1) / BK;
         return all > split ? (all - split + splits - 1) / splits : 0;
     };
-    int it = 0, sets = 0;
+    int it = 0, rt = 0;
     bool live = true;
+    float v[16];
     if (warp == 0) {
         if (lane == 0) {
             for (int item = first; item < items && live; item += stride) {
@@ -535,15 +567,10 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            int lt = 0;
             for (int item = first; item < items && live; item += stride) {
                 const int n = stages(rows_of(g, item / parts));
-                if (n == 0) continue;
-                if (lt > 0) live = x.wait(x.drained, (lt - 1) & 1);
-                ptx::tc_fence_after();
-                live = live && x.template multiply<true>(it, n, (n + T::SETS - 1) / T::SETS);
+                live = x.template multiply<true>(it, rt, n);
                 it += n;
-                ++lt;
             }
             if (!live) {
                 tc_commit_own(x.shutdown);
@@ -554,7 +581,6 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
         const int group = (warp - 2) % kFillGroups, tid = (warp - 2) / kFillGroups * 32 + lane;
         constexpr int PER = BK * R / 8 / T::GROUP_THREADS;  // pieces of 8 values of a thread
         const bool wide = (rank & 3) == 0;
-        int lt = 0;
         for (int item = first; item < items && live; item += stride) {
             const int w = item / parts, col0 = column_of(item), job = job_of(item), width = jobs.width[job];
             const float* c = jobs.c[job];
@@ -577,11 +603,16 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
                 }
             };
             const int mine = (group - it % kFillGroups + kFillGroups) % kFillGroups;  // the group's first stage of this item
+            const int run = T::run_of(n);
+            int drained = 0;  // runs of this item
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = 0.f;
 #pragma unroll
             for (int e = 0; e < PER; ++e) load(mine, e);
             for (int i = mine; i < n; i += kFillGroups) {
                 const int at_ring = it + i, s = at_ring % T::STAGES;
-                if (at_ring >= T::STAGES) live = x.wait_warp(&x.empty[s], ((at_ring / T::STAGES) - 1) & 1, 32);
+                for (; live && i >= (drained + T::SETS) * run; ++drained) live = x.drain(rt++, v);
+                if (live && at_ring >= T::STAGES) live = x.wait_warp(&x.empty[s], ((at_ring / T::STAGES) - 1) & 1, 32);
                 if (!live) break;
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
@@ -608,28 +639,12 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
                 if (lane == 0) ptx::mbar_arrive(&x.filled[s]);
             }
             it += n;
-            sets = 0;
-            if (n > 0 && live) {
-                live = x.wait_warp(x.done, lt & 1, 64);
-                ptx::tc_fence_after();
-                const int run = (n + T::SETS - 1) / T::SETS;
-                sets = (n + run - 1) / run;
-                ++lt;
-            }
+            for (; live && drained * run < n; ++drained) live = x.drain(rt++, v);
             if (!live || splits > 1) break;
-            const int col = col0 + (warp & 3) * 32 + lane;
-            for (int group = (warp - 2) >> 2; group < R / 16; group += T::FILL_WARPS / 4) {
-                float v[16];
-                x.sums(group, sets, v);
+            const int col = col0 + (warp & 3) * 32 + lane, j0 = 16 * ((warp - 2) >> 2);
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (16 * group + j < rank && col < width) G[(size_t)w * ld + jobs.f_off[job] + (size_t)(16 * group + j) * width + col] = jobs.factor[job] * v[j];
-            }
-            if (n > 0) {
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(x.drained);
-            }
+            for (int j = 0; j < 16; ++j)
+                if (j0 + j < rank && col < width) G[(size_t)w * ld + jobs.f_off[job] + (size_t)(j0 + j) * width + col] = jobs.factor[job] * v[j];
         }
     }
     if (splits > 1) {  // one item for each cluster: every block gets its share of the factor's rows from all, over the ring, adds it up and writes it
@@ -638,16 +653,13 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
         float* sums = reinterpret_cast<float*>(x.a);  // [splits][share][BM]
         const int share = R / splits;
         if (warp >= 2) {
-            const int col = (warp & 3) * 32 + lane;
-            for (int group = (warp - 2) >> 2; group < R / 16; group += T::FILL_WARPS / 4) {
-                float v[16];
-                x.sums(group, live ? sets : 0, v);
+            const int col = (warp & 3) * 32 + lane, group = (warp - 2) >> 2;
+            if (group < R / 16)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int r = 16 * group + j;
                     store_to(map_to_block(smem_u32(sums + (split * share + r % share) * BM + col), r / share), v[j]);
                 }
-            }
         }
         cluster_sync();
         const int w = first / parts, col0 = column_of(first), job = job_of(first), width = jobs.width[job];

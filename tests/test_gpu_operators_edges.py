@@ -67,3 +67,63 @@ def test_bad_ranges_of_a_batch_without_rows_are_reported(bad):
         torch.cuda.synchronize()
         assert h.status() == p.STATUS_BAD_INDEX
     assert (q.G[:, q.ad.a_off: q.ad.a_off + 256] == 0).all() and (z.loss == 0).all()
+
+
+# ------------------------------------------------------------------------------------------ adapters
+# Sums over very long axes.  All values are positive, so truncated sums would fall short of the result by a part that grows with the axis: 2^-24 and more
+# of the partial sum at every MMA.  The bounds: a run of at most 32 MMAs, each off by at most a step (2^-23) of the partial sum, whose mean over a run of positive
+# terms is not above its end: 2^-18.  The runs' sums, n of them, are added with rounding, 2^-24 each of a partial sum: n 2^-24 at most for an element; over
+# many elements the roundings cancel, and the mean keeps the truncation's 2^-18.  (Pieces of h, m, l: 2^-26 and less.)
+def _long_sum_close(got, want, runs, what):
+    rel = ((got.double() - want) / want).flatten()
+    assert rel.abs().max().item() <= 2.0 ** -18 + runs * 2.0 ** -24, what
+    assert abs(rel.mean().item()) <= 2.0 ** -18, what
+
+
+def _ramp(shape, seed, dtype=torch.float32):
+    return (0.5 + torch.rand(*shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))).to(dtype)
+
+
+@pytest.mark.parametrize("workers,rank,rows,inp,out", [(1, 64, 9728, 131072, 8), (1, 16, 19200, 131072, 8), (2, 48, 9728, 40000, 8), (160, 8, 160, 131072, 8), (1, 64, 9728, 8, 100000)])
+def test_adapters_sum_over_very_wide_rows(workers, rank, rows, inp, out):
+    """hidden (and, for a wide output, d_hidden) of rows that are one of 128, again and again; too many tiles for the width to be shared by blocks."""
+    import paper_2102_06280_b200 as p
+    wide, down = max(inp, out), out > inp
+    lay = p.lowrank_layout([(inp, out, rank)])
+    ad, h = lay.adapters[0], handle(workers, lay.ld)
+    X = _ramp((workers, lay.ld), 1)
+    few = _ramp((128, wide), 2, torch.bfloat16)
+    v = few.repeat(-(-rows // 128), 1)[:rows]
+    W, other = torch.zeros(out, inp, device="cuda", dtype=torch.bfloat16), torch.zeros(rows, 8, device="cuda", dtype=torch.bfloat16)
+    rs = torch.tensor([rows * w // workers for w in range(workers + 1)], dtype=torch.int32, device="cuda")
+    c, hidden = torch.zeros(rows, rank, device="cuda"), torch.zeros(rows, rank, device="cuda")
+    if down:
+        h.lowrank_backward(ad, X, W, other, hidden, v, rs, torch.zeros_like(X), c)
+    else:
+        h.lowrank_forward(ad, X, W, v, rs, other, c)
+    off = ad.b_off if down else ad.a_off
+    want = torch.empty(rows, rank, device="cuda", dtype=torch.float64)
+    for w in range(workers):
+        F = X[w, off: off + rank * wide].double().view(rank, wide)
+        a, b = int(rs[w]), int(rs[w + 1])
+        want[a:b] = (v[a: min(b, a + 128)].double() @ F.t()).repeat(-(-(b - a) // 128), 1)[: b - a]
+    _long_sum_close(c, want, wide / 512, "hidden")
+    assert h.status() == 0
+
+
+@pytest.mark.parametrize("rank,rows", [(64, 40000), (20, 30000), (48, 33000)])
+def test_adapters_sum_over_very_many_rows(rank, rows):
+    """Gradients of one worker's factors; so many columns that its rows are not shared by blocks."""
+    import paper_2102_06280_b200 as p
+    inp, out = 9600, 9728
+    lay = p.lowrank_layout([(inp, out, rank)])
+    ad, h = lay.adapters[0], handle(1, lay.ld)
+    X, G = torch.zeros(1, lay.ld, device="cuda"), torch.zeros(1, lay.ld, device="cuda")
+    X[:, ad.b_off: ad.b_off + rank * out] = _ramp((1, rank * out), 3) / out
+    x, dy, hidden = _ramp((rows, inp), 4, torch.bfloat16), _ramp((rows, out), 5, torch.bfloat16), _ramp((rows, rank), 6)
+    W, u = torch.zeros(out, inp, device="cuda", dtype=torch.bfloat16), torch.zeros(rows, rank, device="cuda")
+    rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    h.lowrank_backward(ad, X, W, x, hidden, dy, rs, G, u)
+    _long_sum_close(G[0, ad.a_off: ad.a_off + rank * inp].view(rank, inp), u.double().t() @ x.double(), rows / 512, "dA")
+    _long_sum_close(G[0, ad.b_off: ad.b_off + rank * out].view(rank, out), hidden.double().t() @ dy.double(), rows / 512, "dB")
+    assert h.status() == 0
