@@ -7,7 +7,9 @@
 // the projection, whose tiles take the adapter's share along as further steps of their k loop.  All three multiply 16-bit
 // operands on the tensor cores.  x, dy and W are bf16 as they are; an fp32 value v enters as pieces that are bf16 numbers,
 //   v = h + m + l + rest,  h = bf16(v), m = bf16(v - h), l = bf16(v - h - m),  |rest| <= 2^-27 |v|
-// (each difference is exact), so its product with a bf16 value is the fp32 one up to 2^-27.
+// (each difference is exact), so its product with a bf16 value is the fp32 one up to 2^-27.  Where the result is fp32 (hidden, u, dA, dB) the pieces are
+// of 2^24 v: unscaled, l would fall below the smallest bf16 number for |v| < 2^-110.  From 2^104 on the scaled v, or a sum, is infinite or NaN, as it
+// is where an operand is: such a result is summed again on the CUDA cores, in fp32 from the values as they are.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -47,6 +49,32 @@ __device__ __forceinline__ void pieces(float a, float b, uint32_t (&p)[n]) {
         b -= __uint_as_float(p[i] & 0xffff0000u);
     }
 }
+constexpr float kScale = 16777216.f, kUnscale = 1.f / kScale;
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+// Sum of f_k v_k over k < width (a multiple of 8; both begin at multiples of 16 bytes).  A warp.
+__device__ __noinline__ float dot_again(const float* f, const bf16* v, int width) {
+    float sum = 0.f;
+    for (int k = 8 * (threadIdx.x & 31); k < width; k += 256) {
+        const uint4 u = *reinterpret_cast<const uint4*>(v + k);
+        const uint32_t b[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 x = *reinterpret_cast<const float2*>(f + k + 2 * e);
+            sum = fmaf(x.x, __uint_as_float(b[e] << 16), sum);
+            sum = fmaf(x.y, __uint_as_float(b[e] & 0xffff0000u), sum);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+// Sum of c_t v_t over n rows, one value of each.  A thread (its neighbours in a warp take the next v).
+__device__ __noinline__ float column_again(const float* c, int rank, const bf16* v, long long ld_v, int n) {
+    float sum = 0.f;
+    for (int t = 0; t < n; ++t) sum = fmaf(c[(size_t)t * rank], __bfloat162float(v[(size_t)t * ld_v]), sum);
+    return sum;
+}
+
 // d += a b, a 16 x 16 (row major) and b 16 x 8 (column major) of bf16.  Lane l holds of a the values at rows l/4 (registers 0 and 2) and l/4 + 8
 // (1 and 3), k 2(l%4) and the one behind it (0 and 1; 8 further: 2 and 3); of b those at column l/4 and the same k; of d rows l/4
 // and l/4 + 8, columns 2(l%4) and the one behind it.  The k of a product are summed, so any order of them will do, the same in a and b.
@@ -158,8 +186,8 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
             for (int half = 0; half < 2; ++half) {
                 const float4 x = f[j][half];
                 uint32_t b0[3], b1[3];
-                pieces(x.x, x.y, b0);
-                pieces(x.z, x.w, b1);
+                pieces(kScale * x.x, kScale * x.y, b0);
+                pieces(kScale * x.z, kScale * x.w, b1);
                 const uint4 lo = now[0], hi = now[1];
                 const uint32_t a[4] = {half ? lo.z : lo.x, half ? hi.z : hi.x, half ? lo.w : lo.y, half ? hi.w : hi.y};
 #pragma unroll
@@ -195,14 +223,26 @@ __global__ void __launch_bounds__(kShrinkThreads) shrink_kernel(RowGroups g, con
             for (int i = 0; i < NT * 4; ++i) (&acc[0][0])[i] = sum_of_cluster(part + i * 32 + lane, splits);
         cluster_sync();
     }
-    if (split == 0 && warp == 0) {
+    if (split != 0) return;
+    bool odd = false;
+    if (warp == 0) {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int t = range.x + row + (e >> 1) * 8, r = 8 * j + 2 * q + (e & 1);
-                if (t < range.y && r < rank) out[(size_t)t * rank + r] = factor * acc[j][e];
+                if (t >= range.y || r >= rank) continue;
+                if (finite(acc[j][e])) out[(size_t)t * rank + r] = factor * (kUnscale * acc[j][e]);
+                else odd = true;
+                part[(e >> 1) * (8 * NT * 8) + row * (8 * NT) + r] = acc[j][e];  // [16][8 NT]
             }
+    }
+    if (!__syncthreads_or(odd)) return;
+    for (int e = warp; e < (range.y - range.x) * rank; e += kShrinkWarps) {
+        const int t = e / rank, r = e % rank;
+        if (finite(part[t * (8 * NT) + r])) continue;
+        const float sum = dot_again(F + (size_t)r * width, v + (size_t)(range.x + t) * ld_v, width);
+        if (lane == 0) out[(size_t)(range.x + t) * rank + r] = factor * sum;
     }
 }
 
@@ -253,13 +293,13 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
                  : "memory");
     ptx::tc_ld_wait();
 }
-// Three pieces of eight values.
+// Three pieces of 2^24 times eight values.
 __device__ __forceinline__ void split8(const float4& x, const float4& y, uint4 (&p)[3]) {
     uint32_t a[3], b[3], c[3], d[3];
-    pieces(x.x, x.y, a);
-    pieces(x.z, x.w, b);
-    pieces(y.x, y.y, c);
-    pieces(y.z, y.w, d);
+    pieces(kScale * x.x, kScale * x.y, a);
+    pieces(kScale * x.z, kScale * x.w, b);
+    pieces(kScale * y.x, kScale * y.y, c);
+    pieces(kScale * y.z, kScale * y.w, d);
 #pragma unroll
     for (int i = 0; i < 3; ++i) p[i] = make_uint4(a[i], b[i], c[i], d[i]);
 }
@@ -317,13 +357,15 @@ struct Thin {
         tc_fence_after();
         tmem = *slot;
     }
-    __device__ __forceinline__ void finish() {
+    // The end, a barrier: returns whether `p` holds for any thread.
+    __device__ __forceinline__ bool finish(bool p = false) {
         ptx::tc_fence_before();
-        __syncthreads();
+        p = __syncthreads_or(p);
         if (threadIdx.x >> 5 == 1) {
             ptx::tc_fence_after();
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(thin_columns(R)) : "memory");
         }
+        return p;
     }
     __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) const {
         return ptx::mbar_try_wait<false>(bar, parity) || ptx::mbar_wait_bounded<false>(bar, parity, kSpinLimit, 0, abort, status);
@@ -402,7 +444,7 @@ __device__ __forceinline__ void land(const Thin<R>& x, int issued) {
 // 8192 rows, 4096 wide, rank 16: 20 us (67 MB of rows, 10.2 us of the memory; 3.4 TB/s); rank 64: 32 us, where forming the pieces is as long.
 template <int R>
 __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid_constant__ CUtensorMap map_v, RowGroups g, const float* X, long long ld, long long f_off,
-                                                                 int rank, int width, float factor, float* out, int splits) {
+                                                                 int rank, int width, const bf16* rows_v, long long ld_v, float factor, float* out, int splits) {
     using T = Thin<R>;
     extern __shared__ uint8_t raw[];
     if (threadIdx.x == 0) prefetch_map(&map_v);
@@ -415,6 +457,7 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
     x.setup(raw, g.status);
     dependents_may_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = blockIdx.x % splits;
+    const float* F = X + (size_t)w * ld + f_off;
     const int all = (width + BK - 1) / BK, kb0 = (int)((long long)all * split / splits), n = (int)((long long)all * (split + 1) / splits) - kb0;
     bool live = true;
     float v[16];
@@ -443,7 +486,6 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
     } else {
         const int group = (warp - 2) % kFillGroups, tid = (warp - 2) / kFillGroups * 32 + lane;
         constexpr int PER = R * 8 / T::GROUP_THREADS;  // pieces of 8 k of a thread
-        const float* F = X + (size_t)w * ld + f_off;
         float4 f[PER][2];
         auto load = [&](int i, int e) {
             const int at = tid + e * T::GROUP_THREADS, j = at >> 3, k = (kb0 + i) * BK + 8 * (at & 7);
@@ -496,14 +538,27 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
     }
     if (splits > 1) cluster_sync();
     else __syncthreads();
-    for (int e = threadIdx.x; e < share * R; e += T::THREADS) {
-        const int i = e / R, j = e % R, t = range.x + split * share + i;
-        if (t >= range.y || j >= rank) continue;
+    auto sum_of = [&](int i, int j) {
         float sum = sums[i * PITCH + j];
         for (int k = 1; k < splits; ++k) sum += sums[(k * share + i) * PITCH + j];
-        out[(size_t)t * rank + j] = factor * sum;
+        return sum;
+    };
+    bool odd = false;
+    const int first = range.x + split * share;
+    for (int e = threadIdx.x; e < share * R; e += T::THREADS) {
+        const int i = e / R, j = e % R;
+        if (first + i >= range.y || j >= rank) continue;
+        const float sum = sum_of(i, j);
+        if (finite(sum)) out[(size_t)(first + i) * rank + j] = factor * (kUnscale * sum);
+        else odd = true;
     }
-    x.finish();
+    if (x.finish(odd))
+        for (int e = warp; e < min(share, range.y - first) * rank; e += T::THREADS / 32) {
+            const int i = e / rank, j = e % rank;
+            if (finite(sum_of(i, j))) continue;
+            const float sum = dot_again(F + (size_t)j * width, rows_v + (size_t)(first + i) * ld_v, width);
+            if (lane == 0) out[(size_t)(first + i) * rank + j] = factor * sum;
+        }
 }
 
 // ----------------------------------------------------------------------------- outer
@@ -520,6 +575,8 @@ struct OuterJobs {  // of the one factor, and of the other
     int width[2];
     float factor[2];
     const float* c[2];
+    const bf16* v[2];
+    long long ld_v[2];
 };
 template <int R>
 __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_constant__ CUtensorMap map_0, const __grid_constant__ CUtensorMap map_1, RowGroups g, float* G,
@@ -642,9 +699,23 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
             for (; live && drained * run < n; ++drained) live = x.drain(rt++, v);
             if (!live || splits > 1) break;
             const int col = col0 + (warp & 3) * 32 + lane, j0 = 16 * ((warp - 2) >> 2);
+            float* to = G + (size_t)w * ld + jobs.f_off[job] + (size_t)j0 * width + col;
+            float none = 0.f;  // NaN as soon as a sum is not finite
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (j0 + j < rank && col < width) G[(size_t)w * ld + jobs.f_off[job] + (size_t)(j0 + j) * width + col] = jobs.factor[job] * v[j];
+            for (int j = 0; j < 16; ++j) {
+                none = fmaf(0.f, v[j], none);
+                if (j0 + j < rank && col < width) to[(size_t)j * width] = jobs.factor[job] * (kUnscale * v[j]);
+            }
+            if (none != 0.f && col < width) {
+                uint32_t odd = 0;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) odd |= j0 + j < rank && !finite(v[j]) ? 1u << j : 0u;
+                for (; odd; odd &= odd - 1) {
+                    const int j = __ffs(odd) - 1;
+                    to[(size_t)j * width] = jobs.factor[job] * column_again(c + (size_t)r.x * rank + j0 + j, rank, jobs.v[job] + (size_t)r.x * jobs.ld_v[job] + col, jobs.ld_v[job], r.y - r.x);
+                }
+            }
+            __syncwarp();
         }
     }
     if (splits > 1) {  // one item for each cluster: every block gets its share of the factor's rows from all, over the ring, adds it up and writes it
@@ -668,6 +739,12 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
             if (r >= rank || col0 + k >= width) continue;
             float sum = sums[e];
             for (int j = 1; j < splits; ++j) sum += sums[j * share * BM + e];
+            if (finite(sum)) {
+                sum *= kUnscale;
+            } else {
+                const int2 own = rows_of(g, w);
+                sum = column_again(jobs.c[job] + (size_t)own.x * rank + r, rank, jobs.v[job] + (size_t)own.x * jobs.ld_v[job] + col0 + k, jobs.ld_v[job], own.y - own.x);
+            }
             G[(size_t)w * ld + jobs.f_off[job] + (size_t)r * width + col0 + k] = jobs.factor[job] * sum;
         }
     }
@@ -1439,7 +1516,7 @@ int launch_shrink_tc(dbw_handle* h, const RowGroups& g, const float* X, int64_t 
     const int tiles = g.rows / BM + std::min(g.N, g.rows), room = h->sm_count * (thin_columns(R) == 256 ? 2 : 1);
     int splits = 1;
     while (splits < 8 && 2 * splits * (g.rows / BM) <= room && width >= 4 * BK * splits) splits *= 2;
-    launch_clusters(shrink_tc_kernel<R>, tiles * splits, thin_threads(R), splits, thin_smem(R), s, map, g, X, h->ld, f_off, rank, width, factor, out, splits);
+    launch_clusters(shrink_tc_kernel<R>, tiles * splits, thin_threads(R), splits, thin_smem(R), s, map, g, X, h->ld, f_off, rank, width, (const bf16*)v, ld_v, factor, out, splits);
     DBW_LAUNCHED();
     return DBW_OK;
 }
@@ -1472,7 +1549,7 @@ int launch_outer_as(dbw_handle* h, const RowGroups& g, float* G, int rank, const
     if ((rc = allow_smem(outer_tc_kernel<R>, thin_smem(R), once, h->device)) ||
         (g.rows > 0 && ((rc = make_map(&map_a, a.v, a.width, g.rows, a.ld_v, BK)) || (rc = make_map(&map_b, b.v, b.width, g.rows, b.ld_v, BK)))))
         return rc;
-    const OuterJobs jobs{{a.f_off, b.f_off}, {a.width, b.width}, {a.factor, b.factor}, {a.c, b.c}};
+    const OuterJobs jobs{{a.f_off, b.f_off}, {a.width, b.width}, {a.factor, b.factor}, {a.c, b.c}, {(const bf16*)a.v, (const bf16*)b.v}, {a.ld_v, b.ld_v}};
     const int64_t items = (int64_t)g.N * ((a.width + BM - 1) / BM + (b.width + BM - 1) / BM), room = h->sm_count * (thin_columns(R) == 256 ? 2 : 1);
     int splits = 1;
     while (splits < 8 && 2 * splits * items <= room && (int64_t)g.rows >= 2 * (int64_t)g.N * splits * BK) splits *= 2;

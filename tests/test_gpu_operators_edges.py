@@ -127,3 +127,79 @@ def test_adapters_sum_over_very_many_rows(rank, rows):
     _long_sum_close(G[0, ad.a_off: ad.a_off + rank * inp].view(rank, inp), u.double().t() @ x.double(), rows / 512, "dA")
     _long_sum_close(G[0, ad.b_off: ad.b_off + rank * out].view(rank, out), hidden.double().t() @ dy.double(), rows / 512, "dB")
     assert h.status() == 0
+
+
+# The ends of the fp32 range.  Inputs are taken as they are (fp32 or bf16 numbers); a result is off by what its sum of products may be (2 (n + 4) 2^-24 of their
+# magnitudes, as everywhere), and, where it is subnormal, by three roundings to multiples of 2^-149: 2^-148 with the factor 1.5 that multiplies one.
+SMALLEST = 2.0 ** -148
+SHAPES = [([1, 2, 1], 136, 264, 5), ([3, 0, 9, 2], 520, 72, 16), ([1, 2, 4], 264, 200, 33), ([1, 5], 72, 136, 64),      # a few rows to a worker
+          ([40, 130, 7], 136, 264, 5), ([300, 0, 280], 520, 200, 16), ([90, 60], 264, 520, 33), ([200, 70], 72, 136, 64), ([33, 65, 20], 136, 136, 48)]
+
+
+def _put(q, A=None, B=None):
+    for v, off in ((A, q.ad.a_off), (B, q.ad.b_off)):
+        if v is not None:
+            v = v.astype(np.float32)
+            q.X[:, off: off + v[0].size] = dev(v.reshape(q.n, -1))
+            if off == q.ad.a_off:
+                q.A = v
+            else:
+                q.B = v
+
+
+def _check_fp32(q, hidden):
+    """hidden of the forward call; d_hidden, dA and dB of the backward call that is given `hidden`."""
+    f64 = lambda a: np.asarray(a, dtype=np.float64)  # noqa: E731
+    A, B, x, dy, c = f64(q.A), f64(q.B), host(q.x), host(q.dy), f64(hidden)
+    q.forward()
+    got = host(q.hidden)
+    q.backward(hidden=dev(hidden))
+    u, G = host(q.u), host(q.G)
+    with np.errstate(all="ignore"):
+        for w, a, b in ref.ranges(q.rowstart):
+            def one(got, first, second, k, what):
+                want, size = k * (first @ second), abs(k) * (np.abs(first) @ np.abs(second))
+                close(got, want, 2 * (first.shape[1] + 4) * ref.U32 * size + SMALLEST, what)
+            one(got[a:b], x[a:b], A[w].T, 1.0, "hidden")
+            one(u[a:b], dy[a:b], B[w].T, q.scale, "d_hidden")
+            one(G[w, q.ad.a_off: q.ad.a_off + A[w].size].reshape(A[w].shape), u[a:b].T, x[a:b], 1.0, "dA")
+            one(G[w, q.ad.b_off: q.ad.b_off + B[w].size].reshape(B[w].shape), c[a:b].T, dy[a:b], q.scale, "dB")
+    assert q.h.status() == 0
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("size", [1e-32, 1e-36, 1e-38, 3e-42])
+def test_adapters_of_the_smallest_values(shape, size):
+    q = Projection(*shape, seed=1)
+    _put(q, q.A * size, q.B * size)
+    _check_fp32(q, (size * np.random.default_rng(5).standard_normal((q.rows, shape[3]))).astype(np.float32))
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("size", [2e31, 1e37, 2e38])
+def test_adapters_of_the_largest_values(shape, size):
+    """Up to the largest fp32 number; x and dy are so small that no sum passes it."""
+    q, rng, most = Projection(*shape, seed=2), np.random.default_rng(6), np.finfo(np.float32).max
+    q.x *= 2.0 ** -12
+    q.dy *= 2.0 ** -12
+
+    def large(like):
+        v = np.clip(size * rng.standard_normal(like), -float(most), float(most)).astype(np.float32)
+        v.reshape(-1)[:: 17] = most if size > 1e38 else size
+        return v
+    _put(q, large(q.A.shape), large(q.B.shape))
+    _check_fp32(q, large((q.rows, shape[3])))
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_adapters_of_infinite_values(shape):
+    """An infinite value gives what the formula gives: an infinity of its sign where the other factor has one, NaN where two disagree."""
+    q, rng = Projection(*shape, seed=3), np.random.default_rng(7)
+    rank, (w, a, b) = shape[3], max(ref.ranges(q.rowstart), key=lambda r: r[2] - r[1])
+    A, B, hidden = q.A.copy(), q.B.copy(), rng.standard_normal((q.rows, rank)).astype(np.float32)
+    A[w, rank - 1, 7], A[w, 0, 0], B[w, rank // 2, 70], hidden[a, rank - 1] = np.inf, np.nan, -np.inf, np.inf
+    _put(q, A, B)
+    _check_fp32(q, hidden)
+    _put(q, np.ones_like(A), -2 * np.ones_like(B))        # (bf16 numbers: two of their three pieces are 0, and 0 x inf is NaN)
+    q.x[a, 3], q.dy[b - 1, 11] = float("inf"), float("-inf")
+    _check_fp32(q, np.ones_like(hidden))
