@@ -369,7 +369,9 @@ int dbw_lowrank_layout(const int32_t* shapes, int32_t n, dbw_lowrank_desc* desc,
  *             `in` bf16, ld_x elements apart, rowstart.
  * DEVICE out: y [rows] rows of `out` bf16, ld_y elements apart; hidden [rows][rank] fp32 (dbw_lowrank_backward takes it).
  * ld_x and ld_y are multiples of 8; X, W, x, y and hidden begin at multiples of 16 bytes.  bf16 products are exact and the fp32
- * factors enter as sums of bf16 pieces, accumulated in fp32: hidden is an fp32 result, y is one rounding from it.
+ * factors enter as sums of bf16 pieces, accumulated in fp32.  hidden is an fp32 result over the whole range of fp32, d_hidden and the factors' gradients
+ * below too.  y is W x + bias + sum_j (scale hidden_j) B_j, each scale hidden_j rounded to fp32 and the adapter's share good to 2^-16 of
+ * its products (a value of it below 2^-116 to 2^-134), summed in fp32 (truncated every 16 k, by 2^-23 of the partial sum at most) and rounded to bf16.
  * A training batch and a decoding step (a row or a few per worker) are the same call.
  */
 int dbw_lowrank_forward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, const float* X, const void* W,

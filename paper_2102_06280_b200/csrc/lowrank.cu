@@ -767,9 +767,12 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
 //     k:            [0, R)        [R, 2R)      [2R, 3R)         R = rank rounded up to 16
 //     rows:         h of c        l of c       h of c           (v = h + l + rest, |rest| <= 2^-17 |v|)
 //     columns:      h of F        h of F       l of F
-// while the MMAs of the slots before run.  What is left out, l l and the rests, is below 2^-16 of a product; y has 8 bits.
-// An infinite or NaN value of one worker's factor must not reach the rows of another through 0 x inf: such a value enters as
-// zero, and the epilogue adds its products to the rows they belong to on the CUDA cores.
+// while the MMAs of the slots before run.  What is left out, l l and the rests, is below 2^-16 of a product; y has 8 bits.  The sums in
+// tensor memory stay there over the whole k loop and are truncated at every MMA: of one sign, 8e-8 of the sum for 16 k, 2e-5 at K = 4096 (y's
+// half step: 2e-3).
+// An infinite or NaN value of one worker's factor must not reach the rows of another through 0 x inf, and of one value's pieces it would make NaN where
+// the product is infinite: a value of F, or of factor x c, that is not finite or rounds to infinity enters as zero, and the epilogue adds its products to the
+// rows they belong to on the CUDA cores, in fp32.
 constexpr int kProjectThreads = 320, kDrainWarps = 8, kDrainThreads = 32 * kDrainWarps;
 __host__ __device__ constexpr int project_stages(int bn) { return bn == 256 ? 6 : 8; }
 __host__ __device__ constexpr size_t project_stage(int bn) { return (size_t)(BM + bn / 2) * BK * 2; }
@@ -878,33 +881,45 @@ __device__ __forceinline__ bool any_of_drain(bool mine) {
     return any != 0;
 }
 
-// Eight values of c, times the factor, as a piece: h, or l.
-__device__ __forceinline__ uint4 row_piece(const float4 (&v)[2], float factor, bool low) {
-    const float f[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
-    uint32_t o[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        uint32_t p[2];
-        pieces(factor * f[2 * e], factor * f[2 * e + 1], p);
-        o[e] = low ? p[1] : p[0];
-    }
-    return make_uint4(o[0], o[1], o[2], o[3]);
+// Whether f is finite and rounds to a finite bf16 number.
+__device__ __forceinline__ bool fits(float f) { return fabsf(f) < 0x1.ffp127f; }
+__device__ __forceinline__ float larger(float a, float b) {  // of the magnitudes; NaN if one is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return d;
 }
-// Eight values of a worker's factor as a piece.  A value that is not finite, in itself or rounded, becomes 0 and is reported.
-__device__ __forceinline__ uint4 piece8(const float4 (&v)[2], bool low, bool& odd) {
+// Makes the values that do not fit 0; returns whether there were any.  (One comparison of the largest of them: with masks for every value and piece
+// backward_ragged took 45.8 us instead of 43.7.)
+template <int n>
+__device__ __forceinline__ bool without_infinities(float4 (&v)[n][2]) {
+    float most = 0.f;
+#pragma unroll
+    for (int x = 0; x < n; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) most = larger(larger(most, v[x][y].x), larger(v[x][y].y, larger(v[x][y].z, v[x][y].w)));
+    if (fits(most)) return false;
+#pragma unroll
+    for (int x = 0; x < n; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            float4& u = v[x][y];
+            u = make_float4(fits(u.x) ? u.x : 0.f, fits(u.y) ? u.y : 0.f, fits(u.z) ? u.z : 0.f, fits(u.w) ? u.w : 0.f);
+        }
+    return true;
+}
+// Eight values as a piece: h, or l.  (A value below 2^-116 is held to 2^-134, half the smallest bf16 number: times the other factor that is nothing to
+// a bf16 y unless that is 2^100 and more.)
+__device__ __forceinline__ uint4 piece8(const float4 (&v)[2], bool low) {
     const float f[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
     uint32_t o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         uint32_t p[2];
         pieces(f[2 * e], f[2 * e + 1], p);
-        const bool lo_bad = (p[0] & 0x7f80u) == 0x7f80u, hi_bad = (p[0] & 0x7f800000u) == 0x7f800000u;
-        odd |= lo_bad || hi_bad;
-        o[e] = (low ? p[1] : p[0]) & (lo_bad ? 0xffff0000u : 0xffffffffu) & (hi_bad ? 0xffffu : 0xffffffffu);
+        o[e] = low ? p[1] : p[0];
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
-__device__ __forceinline__ bool rounds_to_finite(float f) { return (pack2(f, 0.f) & 0x7f80u) != 0x7f80u; }
 
 template <int BN, bool BMN>
 __global__ void __launch_bounds__(kProjectThreads, 1)
@@ -925,6 +940,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
     volatile uint32_t* abort = tmem_slot + 1;
     volatile uint32_t* odd_flag = tmem_slot + 2;  // [3], a tile's by turns: its factors hold values that are not finite
+    volatile uint32_t* odd_rows = tmem_slot + 5;  // [3], its c, of this block's rows
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();  // 0 = leader of the pair
@@ -934,7 +950,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
     }
     if (threadIdx.x == 0) {
         *abort = 0u;
-        odd_flag[0] = odd_flag[1] = odd_flag[2] = 0u;
+        for (int e = 0; e < 3; ++e) odd_flag[e] = odd_rows[e] = 0u;
         mbar_init(drain, 1);
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&full[s], 2);  // (the leader's) its copies' arrival and one more, or one for each block's pieces
@@ -1119,22 +1135,30 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
             const int own_t = t0 + (int)rank * BM;  // this block's rows
             const int extra = tile_extra, n = num_kb + extra;
             volatile uint32_t* odd = odd_flag + lt % 3;
-            if (tid == 0) odd_flag[(lt + 1) % 3] = 0u;  // its last readers are behind the barrier of the tile before
+            if (tid == 0) odd_flag[(lt + 1) % 3] = odd_rows[(lt + 1) % 3] = 0u;  // its last readers are behind the barrier of the tile before
             // ---- the adapters' ring slots: the values of the next one are on their way while one is written ----
             for (int e = 0; w >= 0 && live; ++e) {
                 const int s = (it + place(e, extra, n)) % STAGES;
-                bool bad = false;
                 uint4 pa[4], pb[BH / 32];
                 const int kc = 64 * b + 8 * (tid & 7);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) pa[x] = row_piece(raw_c[x], a.factor, kc >= R && kc < 2 * R);
+                for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int x = 0; x < BH / 32; ++x) pb[x] = piece8(raw_f[x], 64 * b + tid / (BH / 8) + x * (kDrainThreads * 8 / BH) >= 2 * R, bad);
+                    for (int y = 0; y < 2; ++y) {
+                        float4& u = raw_c[x][y];
+                        u = make_float4(a.factor * u.x, a.factor * u.y, a.factor * u.z, a.factor * u.w);
+                    }
+                const bool bad_row = without_infinities(raw_c), bad = without_infinities(raw_f);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) pa[x] = piece8(raw_c[x], kc >= R && kc < 2 * R);
+#pragma unroll
+                for (int x = 0; x < BH / 32; ++x) pb[x] = piece8(raw_f[x], 64 * b + tid / (BH / 8) + x * (kDrainThreads * 8 / BH) >= 2 * R);
                 if (++b == blocks) {
                     b = 0;
                     w = tile_workers.take(a.g, end);
                 }
                 if (w >= 0) load(tile);
+                if (bad_row) odd_rows[lt % 3] = 1u;
                 if (bad) {
                     *odd = 1u;  // in both blocks: each has rows of every column
                     asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(map_to_block(smem_u32((const void*)odd), rank ^ 1u)), "r"(1u) : "memory");
@@ -1168,7 +1192,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
             }
             tc_fence_after();
             const int t = own_t + quarter * 32 + lane;
-            const bool patch = *odd != 0u;
+            const bool odd_f = *odd != 0u, odd_c = odd_rows[lt % 3] != 0u;
             for (int c = half * (BN / 64); c < (half + 1) * (BN / 64); ++c) {
                 const int nb = n0 + c * 32;
                 if (nb >= a.N) break;
@@ -1184,7 +1208,7 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                 if (a.bias)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] += bias[j];
-                if (patch) {
+                if (odd_f || odd_c) {
                     TileWorkers again(a.g, t0, end);
                     for (int w = again.take(a.g, end); w >= 0; w = again.take(a.g, end)) {
                         const int2 own = rows_of(a.g, w);
@@ -1192,9 +1216,11 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                         for (int j = 0; j < a.rank; ++j) {
                             const float* F = a.X + (size_t)w * a.ld + a.f_off + (size_t)j * a.N + nb;
                             const float ct = a.factor * a.c[(size_t)t * a.rank + j];
+                            const bool whole = !fits(ct);  // it entered as 0: all of its products are missing
+                            if (!whole && !odd_f) continue;
 #pragma unroll
                             for (int x = 0; x < 32; ++x)
-                                if (nb + x < a.N && !rounds_to_finite(F[x])) v[x] = fmaf(ct, F[x], v[x]);
+                                if (nb + x < a.N && (whole || !fits(F[x]))) v[x] = fmaf(ct, F[x], v[x]);
                         }
                     }
                     __syncwarp();
@@ -1361,13 +1387,13 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     f[e] = *reinterpret_cast<const float4*>(F + (size_t)(j + e) * a.N);
-                    ct[e] = c[j + e];
+                    ct[e] = a.factor * c[j + e];
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) add(ct[e], f[e]);
             }
 #pragma unroll 4
-            for (; j < a.rank; ++j) add(c[j], *reinterpret_cast<const float4*>(F + (size_t)j * a.N));
+            for (; j < a.rank; ++j) add(a.factor * c[j], *reinterpret_cast<const float4*>(F + (size_t)j * a.N));
             low[i] = sum;
         }
         if (n > 0) {
@@ -1407,8 +1433,8 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
                 const float4 v = *reinterpret_cast<const float4*>(sums + (s * share + at) * BM + 4 * lane);
                 sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
             }
-            sum = make_float4(fmaf(a.factor, low[i].x, sum.x), fmaf(a.factor, low[i].y, sum.y), fmaf(a.factor, low[i].z, sum.z), fmaf(a.factor, low[i].w, sum.w));
-            *reinterpret_cast<uint2*>(a.y + (size_t)(t0 + t) * a.ld_y + n4) = make_uint2(pack2(sum.x, sum.y), pack2(sum.z, sum.w));
+            *reinterpret_cast<uint2*>(a.y + (size_t)(t0 + t) * a.ld_y + n4) =
+                make_uint2(pack2(sum.x + low[i].x, sum.y + low[i].y), pack2(sum.z + low[i].z, sum.w + low[i].w));
         }
     }
     tc_fence_before();

@@ -203,3 +203,86 @@ def test_adapters_of_infinite_values(shape):
     _put(q, np.ones_like(A), -2 * np.ones_like(B))        # (bf16 numbers: two of their three pieces are 0, and 0 x inf is NaN)
     q.x[a, 3], q.dy[b - 1, 11] = float("inf"), float("-inf")
     _check_fp32(q, np.ones_like(hidden))
+
+
+def _check_bf16(q):
+    """y and dx, each from the hidden and d_hidden that the library has for it.  The bound is the plain forms' (operators_reference.py), without what the hidden
+    values are off by.  scale x hidden is an fp32 number: half a step of the smallest ones, 2^-150, times B; where two bf16 pieces hold it, or a factor, that
+    is 2^-134, times the other.  Products and sums below 2^-126 may be taken as 0 (an adapter's, and W's), and y as a multiple of 2^-133.  From 2^128 (1 - 2^-9) on a
+    value rounds to a bf16 infinity (the largest number is 2^128 (1 - 2^-8)); none lies so near that border that its bound reaches over it.  Where
+    terms of both signs come to 2^126, beside larger ones, their fp32 sum may be an infinity of either sign, NaN or a number, by its order: such an element is not compared."""
+    f64 = lambda a: np.asarray(a, dtype=np.float64)  # noqa: E731
+    A, B, W, x, dy = f64(q.A), f64(q.B), host(q.W), host(q.x), host(q.dy)
+    rank = A.shape[1]
+    q.forward()
+    q.backward()
+    y, hid, dx, u = host(q.y), host(q.hidden), host(q.dx), host(q.u)
+    bias = 0.0 if q.bias is None else host(q.bias)
+    with np.errstate(all="ignore"):
+        for w, a, b in ref.ranges(q.rowstart):
+            def one(got, v, M, c, F, k, more, what):
+                want, low = v @ M + k * (c @ F) + more, abs(k) * (np.abs(c) @ np.abs(F))
+                off = 2 * (len(M) + 3 * rank + 4) * ref.U32 * (np.abs(v) @ np.abs(M) + low + np.abs(more)) + 2.0 ** -16 * low + (abs(k) * rank + len(M)) * 2.0 ** -126
+                off = off + 2.0 ** -134 * ((1 + 2.0 ** -16) * np.abs(F).sum(axis=0) + np.abs(k * c).sum(axis=1, keepdims=True))
+                border = 2.0 ** 128 * (1 - 2.0 ** -9)
+                anything = np.isfinite(want) & (low >= 2.0 ** 127) & (low - np.abs(k * (c @ F)) >= 2.0 ** 126)
+                got, want = np.where(anything, 0.0, got), np.where(anything, 0.0, want)
+                assert not (np.abs(np.abs(want) - border) <= off)[np.isfinite(want) & ~anything].any()
+                want = np.where(np.isfinite(want) & (np.abs(want) >= border), np.copysign(np.inf, want), want)
+                close(got, want, off + ref.U16["bf16"] * (np.abs(want) + off) + 2.0 ** -134, what)
+            one(y[a:b], x[a:b], W.T, hid[a:b], B[w], q.scale, bias, "y")
+            one(dx[a:b], dy[a:b], W, u[a:b], A[w], 1.0, 0.0, "dx")
+    assert q.h.status() == 0
+
+
+# (few rows to a worker; little work; pairs of blocks, tiles of 128 and of 256 columns, workers of several tiles and several workers in one)
+PRODUCTS = [([1, 2, 1], 136, 264, 5), ([40, 130, 7], 136, 264, 5), ([90, 60], 264, 520, 33), ([300, 0, 280, 90], 520, 2000, 16), ([700, 655], 1304, 2600, 33),
+            ([200, 900], 2600, 1000, 64)]
+
+
+@pytest.mark.parametrize("shape", PRODUCTS)
+@pytest.mark.parametrize("a,b", [(1e30, 1e-38), (1e30, 3e-42), (1e-38, 1e30), (3e-42, 1e31), (1e-34, 1.0), (1.0, 1e-34)])
+def test_adapters_share_of_small_and_large_values(shape, a, b):
+    """The adapter's share alone (W is 0): factors of very different sizes, whose products are ordinary numbers."""
+    q = Projection(*shape, seed=4, bias=False)
+    q.W.zero_()
+    _put(q, q.A * a, q.B * b)
+    _check_bf16(q)
+
+
+@pytest.mark.parametrize("shape", PRODUCTS)
+def test_adapters_share_of_a_few_small_large_and_infinite_values(shape):
+    q, rng = Projection(*shape, seed=5), np.random.default_rng(8)
+    A, B = q.A.copy(), q.B.copy()
+    for v in (A, B):                                      # a few values of a factor lie at the ends, most do not
+        n = v.size // 50
+        v.reshape(-1)[rng.choice(v.size, n, replace=False)] = rng.choice([1e-38, 1e-41, 1e-37, 1e25], size=n) * rng.standard_normal(n)
+    _put(q, A, B)
+    _check_bf16(q)
+    most = np.finfo(np.float32).max
+    A, B = q.A.copy() * 0 + 1, q.B.copy() * 0 + 2
+    w = max(ref.ranges(q.rowstart), key=lambda r: r[2] - r[1])[0]
+    A[w, 1, :], B[w, 2, 9], A[w, 3, 60] = 0.0, most, most
+    A[w, 1, 5] = most                                     # of one value of x: hidden = x times it, large but finite for |x| < 1
+    q.x[:, 5] = torch.clamp(q.x[:, 5], -0.99, 0.99)
+    q.x[:, 60] = torch.clamp(q.x[:, 60], -0.25, 0.25)
+    q.dy[:, 9] = torch.clamp(q.dy[:, 9], -0.25, 0.25)
+    B[w, 1, :], B[w, 3, :] = 2.0 ** -20, 2.0 ** -20
+    q.scale = 2.0 ** -4
+    _put(q, A, B)
+    _check_bf16(q)
+
+
+@pytest.mark.parametrize("shape", PRODUCTS)
+def test_adapters_share_of_infinite_hidden_values(shape):
+    """hidden of a row that has overflowed: its y is an infinity of B's sign, not NaN, and only in its row."""
+    q = Projection(*shape, seed=6, bias=False)
+    w, a, b = max(ref.ranges(q.rowstart), key=lambda r: r[2] - r[1])
+    A, B = q.A.copy(), q.B.copy()
+    A[w, 1, 7], B[w, 0, 9] = np.inf, -np.inf              # rows of worker w: hidden[:, 1] is infinite, d_hidden[:, 0] too
+    _put(q, A, B)
+    _check_bf16(q)
+    _put(q, np.ones_like(A), np.ones_like(B))
+    q.x[a, 3], q.dy[b - 1, 11] = float("inf"), float("-inf")
+    q.W.abs_()                                            # of one sign: no infinities that disagree
+    _check_bf16(q)
