@@ -51,10 +51,13 @@ __device__ __forceinline__ void pieces(float a, float b, uint32_t (&p)[n]) {
 }
 constexpr float kScale = 16777216.f, kUnscale = 1.f / kScale;
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
-// Sum of f_k v_k over k < width (a multiple of 8; both begin at multiples of 16 bytes).  A warp.
+// Sum of f_k v_k over k < width (a multiple of 8; both begin at multiples of 16 bytes).  A warp.  NaN stays NaN: it goes no further then, here and below
+// (8192 rows, 4096 <- 4096, rank 64, all workers diverged: 5.8 ms for the backward pass, 11.4 with sums to the end).
 __device__ __noinline__ float dot_again(const float* f, const bf16* v, int width) {
     float sum = 0.f;
-    for (int k = 8 * (threadIdx.x & 31); k < width; k += 256) {
+    for (int k0 = 0; k0 < width && !__any_sync(0xffffffffu, sum != sum); k0 += 256) {
+        const int k = k0 + 8 * (threadIdx.x & 31);
+        if (k >= width) continue;
         const uint4 u = *reinterpret_cast<const uint4*>(v + k);
         const uint32_t b[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -71,7 +74,13 @@ __device__ __noinline__ float dot_again(const float* f, const bf16* v, int width
 // Sum of c_t v_t over n rows, one value of each.  A thread (its neighbours in a warp take the next v).
 __device__ __noinline__ float column_again(const float* c, int rank, const bf16* v, long long ld_v, int n) {
     float sum = 0.f;
-    for (int t = 0; t < n; ++t) sum = fmaf(c[(size_t)t * rank], __bfloat162float(v[(size_t)t * ld_v]), sum);
+    for (int t0 = 0; t0 < n && sum == sum; t0 += 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t0 + i;
+            if (t < n) sum = fmaf(c[(size_t)t * rank], __bfloat162float(v[(size_t)t * ld_v]), sum);
+        }
+    }
     return sum;
 }
 
