@@ -23,7 +23,7 @@ namespace dbw {
 namespace {
 
 typedef __nv_bfloat16 bf16;
-using ptx::smem_u32;
+using namespace ptx;
 
 constexpr int BM = 128, BK = 64;  // rows of an operand tile, and its depth: 128 bytes, one swizzled row
 constexpr uint32_t kSpinLimit = 1u << 24;
@@ -111,10 +111,9 @@ __device__ __forceinline__ void store_to(uint32_t cluster_addr, float v) { asm v
 __device__ __forceinline__ void store_to(uint32_t cluster_addr, float a, float b, float c, float d) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
 }
-// The sum, in the order of the blocks, of the floats that the `n` (at most 8) blocks of the cluster have at this place of their shared memory.  The
+// The sum, in the order of the blocks, of the floats that the `n` (2 to 8) blocks of the cluster have at this place of their shared memory.  The
 // loads are on their way together: one after another they take 0.2 us each.
 __device__ __forceinline__ float sum_of_cluster(const float* p, int n) {
-    if (n == 1) return *p;
     float v[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s)
@@ -282,26 +281,6 @@ __host__ __device__ constexpr size_t thin_smem(int R) { return thin_ring(R) + 10
 __host__ __device__ constexpr uint32_t thin_idesc(int R, bool mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (mn ? 3u << 15 : 0u) | ((uint32_t)(3 * R >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
 }
-__device__ __forceinline__ void tma_load_own(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y),
-                 "r"(smem_u32(bar))
-                 : "memory");
-}
-__device__ __forceinline__ void tc_commit_own(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_mma_own(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-                 : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
-                   "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(taddr)
-                 : "memory");
-    ptx::tc_ld_wait();
-}
 // Three pieces of 2^24 times eight values.
 __device__ __forceinline__ void split8(const float4& x, const float4& y, uint4 (&p)[3]) {
     uint32_t a[3], b[3], c[3], d[3];
@@ -326,7 +305,6 @@ struct Thin {
     uint32_t tmem, *status;
 
     __device__ __forceinline__ void setup(uint8_t* raw, uint32_t* status_word) {
-        using namespace ptx;
         uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
         a = smem;
         b = smem + A_STAGES * A_BYTES;
@@ -388,7 +366,6 @@ struct Thin {
     // The MMAs of `n` stages, from ring position `it` and run number `rt` on.  One thread.
     template <bool MN>
     __device__ __forceinline__ bool multiply(int it, int& rt, int n) const {
-        using namespace ptx;
         const uint64_t da = MN ? mnmajor_sw128_desc(smem_u32(a), 8192) : kmajor_sw128_desc(smem_u32(a));
         const uint64_t db = MN ? mnmajor_sw128_desc(smem_u32(b), 8192) : kmajor_sw128_desc(smem_u32(b));
         constexpr uint64_t STEP = (MN ? 16 * 128 : 16 * 2) / 16;  // 16 further along k: 16 rows of 128 bytes, or 32 bytes inside the swizzle atom
@@ -403,11 +380,11 @@ struct Thin {
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k)
-                tc_mma_own(tmem + set * SET, da + (uint64_t)(sa * (A_BYTES / 16)) + k * STEP, db + (uint64_t)(s * (B_BYTES / 16)) + k * STEP, thin_idesc(R, MN), in_set > 0 || k > 0);
-            tc_commit_own(&empty[s]);
-            tc_commit_own(&used[sa]);
+                tc_mma_bf16(tmem + set * SET, da + (uint64_t)(sa * (A_BYTES / 16)) + k * STEP, db + (uint64_t)(s * (B_BYTES / 16)) + k * STEP, thin_idesc(R, MN), in_set > 0 || k > 0);
+            tc_commit(&empty[s]);
+            tc_commit(&used[sa]);
             if (++in_set == run || i == n - 1) {
-                tc_commit_own(&done[set]);
+                tc_commit(&done[set]);
                 in_set = 0;
                 ++rt;
             }
@@ -482,14 +459,14 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
                     break;
                 }
                 ptx::mbar_expect_tx(&x.landed[s], T::A_BYTES);
-                tma_load_own(x.a + s * T::A_BYTES, &map_v, (kb0 + i) * BK, range.x, &x.landed[s]);
+                tma_load_2d(x.a + s * T::A_BYTES, &map_v, (kb0 + i) * BK, range.x, &x.landed[s]);
             }
             if (!live) land(x, i);
         }
     } else if (warp == 1) {
         int rt = 0;
         if (lane == 0 && !x.template multiply<false>(0, rt, n)) {
-            tc_commit_own(x.shutdown);
+            tc_commit(x.shutdown);
             ptx::mbar_wait_quiet<false>(x.shutdown, 0, 1u << 20);
         }
     } else {
@@ -626,7 +603,7 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
                     }
                     ptx::mbar_expect_tx(&x.landed[s], T::A_BYTES);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) tma_load_own(x.a + s * T::A_BYTES + h * 8192, map, col0 + 64 * h, r.x + (split + i * splits) * BK, &x.landed[s]);
+                    for (int h = 0; h < 2; ++h) tma_load_2d(x.a + s * T::A_BYTES + h * 8192, map, col0 + 64 * h, r.x + (split + i * splits) * BK, &x.landed[s]);
                 }
             }
             if (!live) land(x, it);
@@ -639,7 +616,7 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
                 it += n;
             }
             if (!live) {
-                tc_commit_own(x.shutdown);
+                tc_commit(x.shutdown);
                 ptx::mbar_wait_quiet<false>(x.shutdown, 0, 1u << 20);
             }
         }
@@ -820,20 +797,6 @@ struct Waits {
         return __all_sync(0xffffffffu, ok);
     }
 };
-// into this block's shared memory, counted on a barrier that may be the other block's
-__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)), "l"(map),
-                 "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-// arrives on this barrier of BOTH blocks once all MMAs issued so far are complete (an arrival, no data)
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
-}
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-                 : "memory");
-}
 // kind::f16, D fp32, A and B bf16, M = 256 (two blocks), N = bn; bit 16: B is MN-major
 __host__ __device__ constexpr uint32_t idesc_for(int bn, bool b_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(2 * BM >> 4) << 24);
@@ -933,7 +896,6 @@ __device__ __forceinline__ uint4 piece8(const float4 (&v)[2], bool low) {
 template <int BN, bool BMN>
 __global__ void __launch_bounds__(kProjectThreads, 1)
 project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProjectArgs a) {
-    using namespace ptx;
     constexpr int STAGES = project_stages(BN), BH = BN / 2, A_BYTES = BM * BK * 2, B_BYTES = BH * BK * 2;
     constexpr uint32_t IDESC = idesc_for(BN, BMN), IDESC_MN = idesc_for(BN, true);
     extern __shared__ uint8_t smem_raw[];
@@ -1022,12 +984,12 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                         mbar_arrive(&full[s]);
                     }
                     const uint32_t bar = map_to_block(smem_u32(&full[s]), 0);
-                    tma_load(tiles_a + s * A_BYTES, &map_v, kb * BK, t0 + (int)rank * BM, bar);
+                    tma_load_2d_pair(tiles_a + s * A_BYTES, &map_v, kb * BK, t0 + (int)rank * BM, bar);
                     if (!BMN) {
-                        tma_load(tiles_b + s * B_BYTES, &map_w, kb * BK, n0, bar);
+                        tma_load_2d_pair(tiles_b + s * B_BYTES, &map_w, kb * BK, n0, bar);
                     } else {
 #pragma unroll
-                        for (int c = 0; c < BH / 64; ++c) tma_load(tiles_b + s * B_BYTES + c * 8192, &map_w, n0 + c * 64, kb * BK, bar);
+                        for (int c = 0; c < BH / 64; ++c) tma_load_2d_pair(tiles_b + s * B_BYTES + c * 8192, &map_w, n0 + c * 64, kb * BK, bar);
                     }
                     ++kb;
                 }
@@ -1066,17 +1028,17 @@ project_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                         constexpr uint64_t STEP = (BMN ? 16 * 128 : 16 * 2) / 16, STEP_MN = 16 * 128 / 16;
                         if (i != next) {
 #pragma unroll
-                            for (int k = 0; k < BK / 16; ++k) tc_mma(d, da + (uint64_t)(k * 2), db + k * STEP, IDESC, i > 0 || k > 0);
+                            for (int k = 0; k < BK / 16; ++k) tc_mma_bf16_pair(d, da + (uint64_t)(k * 2), db + k * STEP, IDESC, i > 0 || k > 0);
                         } else {  // an adapter's
                             const int ks = min(4, steps - 4 * (e % blocks));
-                            for (int k = 0; k < ks; ++k) tc_mma(d, da + (uint64_t)(k * 2), db + k * STEP_MN, IDESC_MN, i > 0 || k > 0);
+                            for (int k = 0; k < ks; ++k) tc_mma_bf16_pair(d, da + (uint64_t)(k * 2), db + k * STEP_MN, IDESC_MN, i > 0 || k > 0);
                             next = place(++e, extra, n);
                         }
-                        tc_commit(&empty[s]);  // frees the slot once these MMAs have read it
+                        tc_commit_pair(&empty[s]);  // frees the slot once these MMAs have read it
                     }
-                    if (live) tc_commit(&acc_full[buf]);
+                    if (live) tc_commit_pair(&acc_full[buf]);
                     else {  // shutdown after an expired wait: the MMAs issued so far are complete before tensor memory is freed
-                        tc_commit(drain);
+                        tc_commit_pair(drain);
                         mbar_wait_quiet<true>(drain, 0, 1u << 20);
                     }
                 }
@@ -1277,7 +1239,6 @@ __host__ __device__ constexpr size_t serve_smem(int tok) { return serve_ring(tok
 template <int TOK, bool BMN>
 __global__ void __launch_bounds__(kServeThreads, 1)
 serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProjectArgs a, int splits) {
-    using namespace ptx;
     constexpr int STAGES = serve_stages(TOK), W_BYTES = BM * BK * 2, V_BYTES = TOK * BK * 2, COLUMNS = TOK < 32 ? 32 : TOK;
     constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((BMN ? 1u : 0u) << 15) | ((uint32_t)(TOK >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
     extern __shared__ uint8_t smem_raw[];
@@ -1334,12 +1295,12 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
                 }
                 mbar_expect_tx(&full[s], W_BYTES + V_BYTES);
                 if (!BMN) {
-                    tma_load_own(tiles_w + s * W_BYTES, &map_w, (kb0 + i) * BK, n0, &full[s]);
+                    tma_load_2d(tiles_w + s * W_BYTES, &map_w, (kb0 + i) * BK, n0, &full[s]);
                 } else {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) tma_load_own(tiles_w + s * W_BYTES + c * 8192, &map_w, n0 + 64 * c, (kb0 + i) * BK, &full[s]);
+                    for (int c = 0; c < 2; ++c) tma_load_2d(tiles_w + s * W_BYTES + c * 8192, &map_w, n0 + 64 * c, (kb0 + i) * BK, &full[s]);
                 }
-                tma_load_own(tiles_v + s * V_BYTES, &map_v, (kb0 + i) * BK, t0, &full[s]);
+                tma_load_2d(tiles_v + s * V_BYTES, &map_v, (kb0 + i) * BK, t0, &full[s]);
             }
         }
     } else if (warp == 1) {
@@ -1351,10 +1312,10 @@ serve_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ 
                 if (!wait(&full[s], (i / STAGES) & 1)) break;
                 tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < BK / 16; ++k) tc_mma_own(tmem, dw + (uint64_t)(s * (W_BYTES / 16)) + k * STEP, dv + (uint64_t)(s * (V_BYTES / 16)) + (uint64_t)(k * 2), IDESC, i > 0 || k > 0);
-                tc_commit_own(&empty[s]);
+                for (int k = 0; k < BK / 16; ++k) tc_mma_bf16(tmem, dw + (uint64_t)(s * (W_BYTES / 16)) + k * STEP, dv + (uint64_t)(s * (V_BYTES / 16)) + (uint64_t)(k * 2), IDESC, i > 0 || k > 0);
+                tc_commit(&empty[s]);
             }
-            tc_commit_own(done);  // (after an expired wait too: what was issued is complete before tensor memory is freed)
+            tc_commit(done);  // (after an expired wait too: what was issued is complete before tensor memory is freed)
             mbar_wait_quiet<false>(done, 0, 1u << 20);
         }
     } else {

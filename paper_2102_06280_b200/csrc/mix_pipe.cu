@@ -43,11 +43,6 @@ struct PipeArgs {
     int* panel_rows;
 };
 
-__device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, int c, int row, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)), "l"(map), "r"(c), "r"(row),
-                 "r"(smem_u32(bar))
-                 : "memory");
-}
 
 // Shared memory: the ring of panels, float4 [rows][GS] of x (and of g), then the plan: weights [N][stride], own weights [N], rows [N][stride]
 // and counts [N] as 16-bit numbers.
@@ -79,8 +74,8 @@ __global__ void __launch_bounds__(kThreads, 2) mix_pipe_kernel(const __grid_cons
         mbar_expect_tx(&full[st], (uint32_t)stage);
         for (int b = 0; b < a.boxes; ++b) {
             uint8_t* to = panels + (size_t)st * stage + b * a.box_rows * GS * 16;
-            load_box(to, &map_x, (int)panel * (4 * GS), b * a.box_rows, &full[st]);
-            if (MODE != NO_GRADIENT) load_box(to + matrix, &map_g, (int)panel * (4 * GS), b * a.box_rows, &full[st]);
+            tma_load_2d(to, &map_x, (int)panel * (4 * GS), b * a.box_rows, &full[st]);
+            if (MODE != NO_GRADIENT) tma_load_2d(to + matrix, &map_g, (int)panel * (4 * GS), b * a.box_rows, &full[st]);
         }
     };
     if (tid == 0) {

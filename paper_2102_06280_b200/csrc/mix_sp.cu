@@ -107,20 +107,6 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, c
     if ((threadIdx.x & 31) == 0) ok = mbar_wait_paused(bar, parity, w, pause_ns);
     return __all_sync(0xffffffffu, ok);
 }
-// 2-D tiled TMA load into this CTA's shared memory; the bytes are counted on the barrier at
-// `bar_cluster_addr`, which may belong to the other CTA of the pair (no multicast).
-__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* map, int c0, int c1, uint32_t bar_cluster_addr) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(bar_cluster_addr)
-        : "memory");
-}
-// Arrives on the barrier at this shared-memory offset in BOTH CTAs once all MMAs issued so far are complete
-// (a barrier arrive sent to the two CTAs of the pair; no data moves).
-__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
-}
 // D (+)= A_sparse * B: A compressed 2:4 along K, its metadata in tensor memory at column `meta_col`
 // (the instruction takes the even column and the low bit of the column as a selector).
 __device__ __forceinline__ void tc_mma_sp_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t meta_taddr, uint32_t accumulate) {

@@ -108,30 +108,9 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, c
     if ((threadIdx.x & 31) == 0) ok = mbar_wait_paused(bar, parity, w, pause_ns);
     return __all_sync(0xffffffffu, ok);
 }
-// 2-D tiled TMA load into this CTA's shared memory; the bytes are counted on the barrier at
-// `bar_cluster_addr`, which may belong to the other CTA of the pair (no multicast).
-__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* map, int c0, int c1, uint32_t bar_cluster_addr) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(smem_u32(dst)), "l"(map), "r"(c0), "r"(c1), "r"(bar_cluster_addr)
-        : "memory");
-}
 // asks for one box of a tensor to be brought into L2 (no shared memory, no completion to wait for)
 __device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int c0, int c1) {
     asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(c0), "r"(c1) : "memory");
-}
-// arrives on the barrier at this shared-memory offset in BOTH CTAs once all MMAs issued so far are complete
-__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
-}
-__device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(kIdesc), "r"(accumulate)
-        : "memory");
 }
 // MN-major piece tiles of this file: chunks of 64 columns x kKB K rows
 __device__ __forceinline__ uint64_t mnmajor_desc(uint32_t smem_addr) { return mnmajor_sw128_desc(smem_addr, kKB * 128); }
@@ -293,8 +272,8 @@ mix_tc_kernel(const __grid_constant__ CUtensorMap tmS, const __grid_constant__ C
                                 const uint64_t db = mnmajor_desc(baseB + pc * kPieceBytes);
 #pragma unroll
                                 for (int k = 0; k < kKB / 16; ++k)  // 16 inputs further: 32 bytes (K-major), 16 rows of 128 bytes (MN-major)
-                                    tc_mma_pair(tmem_base + (uint32_t)(t * kPanel), da + (uint64_t)(k * 2), db + (uint64_t)(k * 128),
-                                                (kc > 0 || hb > 0 || pc > 0 || k > 0) ? 1u : 0u);
+                                    tc_mma_bf16_pair(tmem_base + (uint32_t)(t * kPanel), da + (uint64_t)(k * 2), db + (uint64_t)(k * 128), kIdesc,
+                                                     (kc > 0 || hb > 0 || pc > 0 || k > 0) ? 1u : 0u);
                             }
                             if (kc == a.n_kc - 1 && hb == kKC / kKB - 1) tc_commit_pair(&bars->acc_full[t]);
                         }

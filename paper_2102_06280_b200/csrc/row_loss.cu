@@ -51,7 +51,6 @@ enum { DISTILL = 0, POLICY = 1 };
 template <class T>
 struct Vec {  // 16-bit types: eight values
     static constexpr int n = 8;
-    static __device__ __forceinline__ float one(const T* p) { return (float)*p; }
     static __device__ __forceinline__ void load(uint4 u, float (&v)[8]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -103,7 +102,6 @@ __device__ __forceinline__ uint32_t Vec<__half>::pack(float lo, float hi) {
 template <>
 struct Vec<float> {
     static constexpr int n = 4;
-    static __device__ __forceinline__ float one(const float* p) { return *p; }
     static __device__ __forceinline__ void load(uint4 u, float (&v)[4]) {
         v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
     }
