@@ -286,3 +286,65 @@ def test_adapters_share_of_infinite_hidden_values(shape):
     q.x[a, 3], q.dy[b - 1, 11] = float("inf"), float("-inf")
     q.W.abs_()                                            # of one sign: no infinities that disagree
     _check_bf16(q)
+
+
+# ------------------------------------------------------------------------------------------ together, as they are used
+def test_a_policy_step_and_its_round():
+    """A projection with adapters, two policy losses of its logits (the first's log-probabilities are the second's old ones), the gradient into G and the round
+    that mixes the adapters; from the launches and from a graph."""
+    import paper_2102_06280_b200 as p
+    from oracle import dbw_oracle as orc
+    from workloads import configs as wl
+    rng, rank, inp, vocab = np.random.default_rng(12), 8, 136, 1000
+    rowptr, col = wl.ring(5)
+    lay = p.lowrank_layout([(inp, vocab, rank)])
+    ad, h = lay.adapters[0], p.Dbw(rowptr, col, d=lay.ld)
+    rowstart = np.concatenate([[0], np.cumsum([30, 4, 0, 170, 60])]).astype(np.int32)
+    rows, rs = int(rowstart[-1]), dev(rowstart)
+    X = torch.zeros(5, lay.ld, device="cuda")
+    X[:, ad.a_off: ad.a_off + rank * inp] = dev(rng.standard_normal((5, rank * inp)).astype(np.float32)) / inp ** 0.5
+    X[:, ad.b_off: ad.b_off + rank * vocab] = dev(rng.standard_normal((5, rank * vocab)).astype(np.float32)) * 0.3
+    W, x = (dev(rng.standard_normal((vocab, inp))) / inp ** 0.5).bfloat16(), dev(rng.standard_normal((rows, inp))).bfloat16()
+    action, adv, weight = rng.integers(0, vocab, size=rows).astype(np.int32), rng.standard_normal(rows).astype(np.float32), (rng.random(rows) > 0.2).astype(np.float32)
+    action_d, adv_d, weight_d = dev(action), dev(adv), dev(weight)
+    f32 = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    z, d, dx = (torch.zeros(rows, n, device="cuda", dtype=torch.bfloat16) for n in (vocab, vocab, inp))
+    hidden, u, G, out, old, logp, row, loss = f32(rows, rank), f32(rows, rank), torch.zeros_like(X), torch.zeros_like(X), f32(rows), f32(rows), f32(rows), f32(5)
+    times, b = 1.0 + rng.exponential(size=5), np.ones(5, dtype=np.int32)
+    td, bd, kept, lr = dev(times), dev(b), torch.zeros(len(col), dtype=torch.uint8, device="cuda"), 0.25
+    first_old = torch.full((rows,), -6.0, device="cuda")
+
+    def step():
+        h.lowrank_forward(ad, X, W, x, rs, z, hidden, scale=2.0)
+        h.policy_loss(z, action_d, first_old, adv_d, rs, row, logp=old, row_weight=weight_d)
+        h.policy_loss(z, action_d, old, adv_d, rs, row, loss=loss, logp=logp, d_logits=d, ref_logp=first_old, kl_coef=0.05, temperature=1.25, row_weight=weight_d)
+        h.lowrank_backward(ad, X, W, x, hidden, d, rs, G, u, d_in=dx, scale=2.0)
+        h.round(X, td, bd, lr, out, kept, G_ext=G)
+
+    step()
+    f = lambda v: np.float64(np.float32(v))  # noqa: E731
+    args = (rowstart, weight.astype(np.float64), "bf16")
+    a64, six = adv.astype(np.float64), np.full(rows, -6.0)
+    was = ref.policy(host(z), action, six, None, a64, 1.0, f(0.2), f(0.2), 0.0, *args)
+    close(host(old), was[6], was[7], "log-probabilities of the first loss")
+    want = ref.policy(host(z), action, host(old), six, a64, 1.25, f(0.2), f(0.2), f(0.05), *args)
+    close(host(loss), want[2], want[3], "loss")
+    close(host(d), want[4], want[5], "d_logits")
+    A, B = host(X[:, ad.a_off: ad.a_off + rank * inp]).reshape(5, rank, inp), host(X[:, ad.b_off: ad.b_off + rank * vocab]).reshape(5, rank, vocab)
+    dA, eA, dB, eB, *_ = ref.lowrank_backward(A, B, host(W), host(x), host(hidden), host(d), rowstart, 2.0)
+    close(host(G[:, ad.a_off: ad.a_off + rank * inp]), dA.reshape(5, -1), eA.reshape(5, -1), "dA")
+    close(host(G[:, ad.b_off: ad.b_off + rank * vocab]), dB.reshape(5, -1), eB.reshape(5, -1), "dB")
+    r = orc.dbw_round(rowptr, col, host(X), times, b, lr, G=host(G))
+    assert np.array_equal(kept.cpu().numpy(), r["kept"])
+    assert (np.abs(host(out) - r["X"]).max(axis=1) / np.abs(r["X"]).max(axis=1)).max() <= 1e-5   # the bar of the mix kernels' own tests
+    first = [v.clone() for v in (z, old, logp, loss, d, G, dx, out)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for v in (z, old, logp, loss, d, G, dx, out):
+        v.zero_()
+    for _ in range(3):
+        graph.replay()
+        for v, w in zip((z, old, logp, loss, d, G, dx, out), first):
+            assert torch.equal(v, w)
+    assert h.status() == 0
