@@ -394,7 +394,8 @@ int dbw_lowrank_backward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, 
 
 /*
  * Losses over a vocabulary, beside the softmax cross-entropy of dbw_grad.  Common to both:
- * DEVICE in : logits [rows] rows of `vocab` values of `type` (DBW_TYPE_*), ld elements apart; rowstart; row_weight [rows]
+ * DEVICE in : logits [rows] rows of `vocab` values of `type` (DBW_TYPE_*; DBW_TYPE_BF16 where they are dbw_lowrank_forward's y and their gradient
+ *             dbw_lowrank_backward's dy), ld elements apart; rowstart; row_weight [rows]
  *             fp32 (nullable: 1 / rows of the worker, the mean of its rows).  A row of weight 0 counts nothing: its loss and
  *             gradient are 0 whatever its inputs hold (NaN included), and its logits are not read.
  * DEVICE out: row_loss [rows] fp32, before weighting; loss [N] fp32 (nullable): sum of weight x row_loss over worker w's rows, 0
@@ -411,7 +412,8 @@ int dbw_lowrank_backward(dbw_handle* h, const dbw_lowrank_desc* a, float scale, 
  *     d row_loss / d logit_v = temperature (q_v - sum over the entries j with top_idx_j = v of p_j).
  *   top_idx [rows][top] int32, top_logit [rows][top] fp32, top 1 .. DBW_DISTILL_MAX_TOP.  An entry of index -1 is no entry
  *   (a shorter list); any other index outside [0, vocab) is taken as -1 and sets DBW_STATUS_BAD_INDEX.  An index may occur
- *   twice: both entries count.  A row without an entry has loss and gradient 0.
+ *   twice: both entries count.  A row without an entry has loss and gradient 0.  top = 1 at temperature 1 is the softmax cross-entropy of that index
+ *   (of a next token, say).
  *
  * dbw_policy_loss: the clipped policy objective with a KL term.  With action a, logp = log q_a, ratio = exp(logp - old_logp),
  *     row_loss = -min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(ref_logp - logp) - (ref_logp - logp) - 1);

@@ -427,7 +427,7 @@ __device__ __forceinline__ void land(const Thin<R>& x, int issued) {
 // ----------------------------------------------------------------------------- shrink, many rows
 // c_t = factor (F_w v_t) as above, 128 rows of one worker to a block (rows of others may come along in its copies: every row of the product
 // is its own, theirs are not stored).  The blocks of a cluster share the width.
-// 8192 rows, 4096 wide, rank 16: 20 us (67 MB of rows, 10.2 us of the memory; 3.4 TB/s); rank 64: 32 us, where forming the pieces is as long.
+// 8192 rows, 4096 wide, rank 16: 20 us (67 MB of rows, 10.2 us of the memory; 3.4 TB/s); rank 64: 34 us, where forming the pieces is as long.
 template <int R>
 __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid_constant__ CUtensorMap map_v, RowGroups g, const float* X, long long ld, long long f_off,
                                                                  int rank, int width, const bf16* rows_v, long long ld_v, float factor, float* out, int splits) {
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(thin_threads(R)) shrink_tc_kernel(const __grid
 // transposition anywhere), the pieces of c its columns.  Rows behind the worker's last are zeros in c and, since they
 // may hold anything, are made zeros in v's last stage too.  Where there are fewer items than SMs the blocks of a cluster share an item's rows
 // and add their sums in a fixed order; otherwise a block walks items.
-// Both factors of a projection 4096 -> 4096, 8192 rows, rank 64: 65 us (134 MB of rows, 20.5 us of the memory; forming the pieces of
+// Both factors of a projection 4096 -> 4096, 8192 rows, rank 64: 69 us (134 MB of rows, 20.5 us of the memory; forming the pieces of
 // c anew for every 128 columns is what it spends the rest on).  With a launch for each factor, backwards of little work took 5 to 8 us more.
 struct OuterJobs {  // of the one factor, and of the other
     long long f_off[2];
@@ -744,9 +744,9 @@ __global__ void __launch_bounds__(thin_threads(R)) outer_tc_kernel(const __grid_
 // 128 of the rows and, as an operand, half of the columns, so that a step of the k loop brings (128 + BN / 2) x 64 values into each.
 // Warp 0 streams tiles of v and W by TMA through a ring of STAGES slots (128-byte swizzle, no multicast; the copies of both blocks
 // are counted on the leader's barriers), one thread of the leader's warp 1 issues the MMAs into one of two accumulators in tensor
-// memory, warps 2 to 9 drain the finished one.  (128 x 256 tiles of single blocks, 48 KB a step for the same products, were bound by
-// what L2 delivers: 8192 rows, 4096 -> 4096: 293 us; in pairs 193 us with rank 16 (215 on another board), 1.43 PFLOP/s, bound by the
-// tensor cores.)
+// memory, warps 2 to 9 drain the finished one.  (8192 rows, 4096 -> 4096: 128 x 256 tiles of single blocks, 48 KB a step for the same products, 293 us;
+// in pairs 193 to 212 us with rank 16, by the board, 1.3 to 1.43 PFLOP/s.  No unit is full: tensor cores active 67 % of the cycles, L2 at 40 % of its rate, memory
+// at 9 %; that fewer bytes a step made it faster says that it waits for the tiles on their way from L2.)
 //
 // A tile's rows are the batch's, whosever they are.  The adapters join as further slots, spread over the k loop: for every worker
 // with rows in the tile, warps 2 to 9 fill slots with the pieces of factor x c_t (zeros in the rows of others) and of the worker's factor,

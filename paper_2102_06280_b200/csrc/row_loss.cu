@@ -490,8 +490,9 @@ __global__ void __launch_bounds__(kThreads) short_row_kernel(const __grid_consta
 // the rows of all blocks have room.  Every thread streams its pieces through AHEAD buffers of its own in shared memory (cp.async; nobody
 // else reads them, so no barrier is involved), into the second pass while the sums are joined.
 //
-// 4096 rows of bf16 values: 128000 a row, policy loss: 429 us, 4.9 TB/s; 131072, distillation with a teacher's 64 entries: 457 us, 4.7 TB/s.  What
-// bounds it is memory, half of it written, with the exponentials (two a value: 66 % of what their pipe can do) close behind.
+// 4096 rows of bf16 values: 128000 a row, policy loss: 432 us, 4.9 TB/s; 131072, distillation with a teacher's 64 entries: 451 us, 4.8 TB/s.  Neither
+// memory (60 % of its peak, half of it written) nor the exponentials (two a value: 72 and 65 % of what their pipe can do) is full: a row's phases, and
+// memory that turns from reading to writing, leave some of both.
 //
 // What was slower, 4096 rows of 128000: a row in the registers of a cluster's blocks, 750 us (nothing overlaps a row's phases);
 // a row in a ring of bulk copies of one or two blocks an SM over clusters of two or four, 744 us and more (the exchange of sums, and
